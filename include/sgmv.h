@@ -359,6 +359,72 @@ int sgmv_plan_shrink(const sgmv_problem* p, int32_t n_segs, sgmv_plan* plan);
  * (operand preparation, MFMA expand) for long segments with a workspace.  Host-only, pure. */
 int sgmv_plan_expand(const sgmv_problem* p, int32_t n_segs, sgmv_plan* plan);
 
+/* ---------------------------------------------------------------------------------------------
+ * The 8-bit backbone next to the add-ons.
+ *
+ * The add-ons land on the outputs of a layer's dense projections.  These calls produce them where
+ * the model's own weights and the activations in front of them are held in 8-bit integers with a
+ * scale per output channel and per token row, while the add-ons stay in 16 bits:
+ *
+ *   sgmv_rms_norm_q8   x (+ residual) -> sum, normed rows in 16 bits (the add-ons' x) and in 8 bits
+ *   sgmv_dense_q8      8-bit rows -> y of up to 8 projections;  then sgmv_add_lora(_multi) onto y
+ *   sgmv_silu_mul_q8   gate, up (their add-ons in them) -> rows in 16 bits and in 8 bits
+ *   sgmv_quantize_q8   16-bit rows (the attention's output) -> 8 bits
+ *
+ * Conventions beyond the general ones above:
+ *   - 8-bit rows are int8 [n_tokens][h] with fp32 scales [n_tokens]: they stand for q * scale.
+ *     For row values v, top = max |v|: scale = top / 127 and q = v * (127 / top) rounded to the
+ *     nearest, ties to even, so |q| <= 127.  A row of zeros has scale 0 and zeros.  A row in which
+ *     a value is not finite has scale NaN and zeros, so every product with it is NaN.
+ *   - Between the 16-bit loads and the stores everything is fp32, each output rounded once.
+ *   - 16-bit rows and 8-bit rows are 16-byte aligned, q_scales 4-byte, w_scales and weights
+ *     16-byte (else SGMV_ERR_ALIGN); widths are positive multiples of 8, in the row calls at most
+ *     32768 (else SGMV_ERR_UNSUPPORTED).  n_tokens == 0 returns SGMV_OK and enqueues nothing.
+ *   - Buffers that a call writes must not overlap one another or what it reads, except where said.
+ *   - Calls are asynchronous on `stream`, which belongs to the current device, like the buffers. */
+
+/* Root-mean-square norm with the residual's addition:
+ *   s = x + residual;   sum = s;   n = s * weight / sqrt(mean(s^2) + eps);   out = n;   q = 8 bits of n
+ *   out       device 16-bit [n_tokens][h] or NULL
+ *   q, q_scales  device int8 [n_tokens][h] and fp32 [n_tokens], or both NULL (not with out NULL too)
+ *   sum       device 16-bit [n_tokens][h] or NULL; may be the residual or x itself (in place)
+ *   residual  device 16-bit [n_tokens][h] or NULL (s = x)
+ *   weight    device 16-bit [h];  eps finite and not negative (else SGMV_ERR_UNSUPPORTED)
+ * out may be x, or the residual, where sum is not.  The norm is taken of the fp32 s, not of the
+ * rounded sum. */
+int sgmv_rms_norm_q8(int32_t dtype, void* out, int8_t* q, float* q_scales, void* sum, const void* x,
+                     const void* residual, const void* weight, float eps, int32_t n_tokens, int32_t h,
+                     void* stream);
+
+/* Gated activation, n = gate / (1 + exp(-gate)) * up, out = n, q = 8 bits of n; the arguments as above
+ * (out or q with q_scales may be NULL, not both).  out may be gate or up. */
+int sgmv_silu_mul_q8(int32_t dtype, void* out, int8_t* q, float* q_scales, const void* gate, const void* up,
+                     int32_t n_tokens, int32_t h, void* stream);
+
+/* 16-bit rows x [n_tokens][h] in 8 bits. */
+int sgmv_quantize_q8(int32_t dtype, int8_t* q, float* q_scales, const void* x, int32_t n_tokens, int32_t h,
+                     void* stream);
+
+/* Dense projections of the same 8-bit rows:
+ *   y_i[t][c] = (sum_j q[t][j] * w_i[c][j]) * q_scales[t] * w_scales_i[c],   i < n_proj <= 8
+ * The sum is an exact 32-bit integer, scaled in fp32 and rounded once when y is stored (y is
+ * written, not accumulated into).
+ *   ys        HOST array of device pointers, y_i 16-bit [n_tokens][h_outs[i]], distinct
+ *   q, q_scales  device, as above, width h_in, at most 131064 (else SGMV_ERR_UNSUPPORTED); any int8
+ *             values (-128 too)
+ *   ws        HOST array of device pointers, w_i int8 [h_outs[i]][h_in] (an output channel's weights
+ *             in a row)
+ *   w_scales  HOST array of device pointers, fp32 [h_outs[i]]
+ *   h_outs    HOST array of output widths
+ *   workspace device scratch, 256-byte aligned, or NULL with 0 bytes.  Shapes with few output tiles
+ *             and a long h_in divide the sum over more workgroups where their partial sums fit in it;
+ *             SGMV_DENSE_WORKSPACE_BYTES is enough for every shape.  It needs no preparation, keeps
+ *             nothing between calls, and calls that share it must be ordered. */
+#define SGMV_DENSE_WORKSPACE_BYTES ((size_t)16 << 20)
+int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* q, const float* q_scales,
+                  const int8_t* const* ws, const float* const* w_scales, int32_t n_tokens, int32_t h_in,
+                  const int32_t* h_outs, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid, not part of the operator: enqueue one plain kernel of known traffic on
  * `stream`, for the benchmark's attainable-bandwidth figure and for scaling a profiler's HBM
  * byte counters (the roofline analysis of the paper's microbenchmark section compares the

@@ -103,6 +103,17 @@ def _load():
     L.sgmv_add_lora_multi.argtypes = [P, c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
                                       c.c_void_p, c.c_int32, c.c_int32, c.c_float, c.c_void_p]
     L.sgmv_add_lora_multi.restype = c.c_int
+    L.sgmv_rms_norm_q8.argtypes = [c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
+                                   c.c_void_p, c.c_float, c.c_int32, c.c_int32, c.c_void_p]
+    L.sgmv_rms_norm_q8.restype = c.c_int
+    L.sgmv_silu_mul_q8.argtypes = [c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int32,
+                                   c.c_int32, c.c_void_p]
+    L.sgmv_silu_mul_q8.restype = c.c_int
+    L.sgmv_quantize_q8.argtypes = [c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int32, c.c_int32, c.c_void_p]
+    L.sgmv_quantize_q8.restype = c.c_int
+    L.sgmv_dense_q8.argtypes = [c.c_int32, c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
+                                c.c_int32, c.c_int32, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+    L.sgmv_dense_q8.restype = c.c_int
     L.sgmv_probe.argtypes = [c.c_int, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
     L.sgmv_probe.restype = c.c_int
     L.sgmv_plan_add_lora.argtypes = [P, c.c_int32, c.c_int32, c.POINTER(SgmvPlan)]
@@ -172,6 +183,7 @@ def sgmv_validate_segments(host_seg_starts, n_segs: int, n_tokens: int) -> int:
 
 STATIC_SCRATCH_BYTES = 9 << 20
 STATIC_MAX_WORKSPACE_BYTES = 8 << 20
+DENSE_WORKSPACE_BYTES = 16 << 20
 
 
 class ArgumentError(ctypes.ArgumentError, TypeError):
@@ -225,6 +237,31 @@ class _General:
                      arr(*[_addr(a) for a in xs]), arr(*[_addr(a) for a in A_ptrs]), arr(*[_addr(a) for a in B_ptrs]),
                      _addr(seg_starts), n_segs, layer_idx, scale, _stream(stream))
 
+    @staticmethod
+    def sgmv_rms_norm_q8(dtype: int, out, q, q_scales, sum, x, residual, weight, eps: float, n_tokens: int, h: int, stream=None,
+                         check: bool = True) -> int:
+        return _call("sgmv_rms_norm_q8", check, dtype, _addr(out), _addr(q), _addr(q_scales), _addr(sum), _addr(x),
+                     _addr(residual), _addr(weight), eps, n_tokens, h, _stream(stream))
+
+    @staticmethod
+    def sgmv_silu_mul_q8(dtype: int, out, q, q_scales, gate, up, n_tokens: int, h: int, stream=None, check: bool = True) -> int:
+        return _call("sgmv_silu_mul_q8", check, dtype, _addr(out), _addr(q), _addr(q_scales), _addr(gate), _addr(up), n_tokens,
+                     h, _stream(stream))
+
+    @staticmethod
+    def sgmv_quantize_q8(dtype: int, q, q_scales, x, n_tokens: int, h: int, stream=None, check: bool = True) -> int:
+        return _call("sgmv_quantize_q8", check, dtype, _addr(q), _addr(q_scales), _addr(x), n_tokens, h, _stream(stream))
+
+    @staticmethod
+    def sgmv_dense_q8(dtype: int, ys, q, q_scales, ws, w_scales, n_tokens: int, h_in: int, h_outs, workspace=None,
+                      workspace_bytes: int = 0, stream=None, check: bool = True) -> int:
+        """``ys, ws, w_scales, h_outs`` are sequences, one entry per projection."""
+        n = len(ys)
+        arr = ctypes.c_void_p * n
+        return _call("sgmv_dense_q8", check, dtype, n, arr(*[_addr(a) for a in ys]), _addr(q), _addr(q_scales),
+                     arr(*[_addr(a) for a in ws]), arr(*[_addr(a) for a in w_scales]), n_tokens, h_in,
+                     (ctypes.c_int32 * n)(*h_outs), _addr(workspace), workspace_bytes, _stream(stream))
+
 
 def _calls():
     """The per-layer calls, their usual arguments marshalled in C (csrc/call_module.c)."""
@@ -233,14 +270,16 @@ def _calls():
     except ImportError as e:
         raise ImportError(f"{_HERE} holds no _sgmv_call module for this interpreter: build it with "
                           "`python -m paper_2310_18547_amd.build`") from e
-    names = ("sgmv_shrink", "sgmv_expand", "sgmv_add_lora", "sgmv_add_lora_static", "sgmv_add_lora_multi")
+    names = ("sgmv_shrink", "sgmv_expand", "sgmv_add_lora", "sgmv_add_lora_static", "sgmv_add_lora_multi",
+             "sgmv_rms_norm_q8", "sgmv_silu_mul_q8", "sgmv_quantize_q8", "sgmv_dense_q8")
     size = module.bind(SgmvProblem, SgmvError, tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names),
                        tuple(getattr(_General, n) for n in names))
     assert size == ctypes.sizeof(SgmvProblem)
     return [getattr(module, n) for n in names]
 
 
-sgmv_shrink, sgmv_expand, sgmv_add_lora, sgmv_add_lora_static, sgmv_add_lora_multi = _calls()
+(sgmv_shrink, sgmv_expand, sgmv_add_lora, sgmv_add_lora_static, sgmv_add_lora_multi,
+ sgmv_rms_norm_q8, sgmv_silu_mul_q8, sgmv_quantize_q8, sgmv_dense_q8) = _calls()
 
 
 def sgmv_plan_expand(p: SgmvProblem, n_segs: int, check: bool = True):

@@ -28,16 +28,26 @@ typedef int (*add_lora_fn)(const sgmv_problem*, void*, const void*, const void* 
 typedef int (*add_lora_multi_fn)(const sgmv_problem*, int32_t, void* const*, const void* const*,
                                  const void* const* const*, const void* const* const*, const int32_t*, int32_t,
                                  int32_t, float, void*);
+typedef int (*rms_norm_fn)(int32_t, void*, int8_t*, float*, void*, const void*, const void*, const void*, float, int32_t,
+                           int32_t, void*);
+typedef int (*silu_mul_fn)(int32_t, void*, int8_t*, float*, const void*, const void*, int32_t, int32_t, void*);
+typedef int (*quantize_fn)(int32_t, int8_t*, float*, const void*, int32_t, int32_t, void*);
+typedef int (*dense_fn)(int32_t, int32_t, void* const*, const int8_t*, const float*, const int8_t* const*, const float* const*,
+                        int32_t, int32_t, const int32_t*, void*, size_t, void*);
 
 static shrink_fn fn_shrink;
 static expand_fn fn_expand;
 static add_lora_fn fn_add_lora;
 static add_lora_fn fn_add_lora_static;
 static add_lora_multi_fn fn_add_lora_multi;
+static rms_norm_fn fn_rms_norm;
+static silu_mul_fn fn_silu_mul;
+static quantize_fn fn_quantize;
+static dense_fn fn_dense;
 static PyObject* problem_type;  // binding.SgmvProblem
 static PyObject* error_type;    // binding.SgmvError
-static PyObject* general[5];    // the functions in Python, in the order of bind()'s addresses
-enum { SHRINK, EXPAND, ADD_LORA, ADD_LORA_STATIC, ADD_LORA_MULTI };
+enum { SHRINK, EXPAND, ADD_LORA, ADD_LORA_STATIC, ADD_LORA_MULTI, RMS_NORM, SILU_MUL, QUANTIZE, DENSE, CALLS };
+static PyObject* general[CALLS];  // the functions in Python, in the order of bind()'s addresses
 static PyObject *str_data_ptr, *str_cuda_stream;
 
 // What the conversions below return besides an error (-1, an exception is set): the value is there, or
@@ -283,27 +293,156 @@ static PyObject* call_add_lora_multi(PyObject* self, PyObject* const* args, Py_s
   return finish(rc, g[10], "sgmv_add_lora_multi");
 }
 
-// bind(problem type, error type, then of sgmv_shrink, sgmv_expand, sgmv_add_lora, sgmv_add_lora_static
-// and sgmv_add_lora_multi the addresses and the functions in Python)
+static PyObject* call_rms_norm(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"dtype", "out",    "q",   "q_scales", "sum", "x",      "residual",
+                                      "weight", "eps", "n_tokens", "h",   "stream", "check"};
+  PyObject* g[13];
+  void* a[7];  // out .. weight
+  void* stream;
+  int32_t dtype, n_tokens, h;
+  float eps;
+  int rc = sort_arguments(names, 13, 11, args, nargs, kwnames, g);
+  FIRST(int32_of(g[0], &dtype));
+  for (int i = 0; i < 7; ++i) FIRST(address_of(g[1 + i], &a[i]));
+  FIRST(float_of(g[8], &eps));
+  FIRST(int32_of(g[9], &n_tokens));
+  FIRST(int32_of(g[10], &h));
+  FIRST(stream_of(g[11], &stream));
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[RMS_NORM], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_rms_norm(dtype, a[0], (int8_t*)a[1], (float*)a[2], a[3], a[4], a[5], a[6], eps, n_tokens, h, stream);
+  Py_END_ALLOW_THREADS
+  return finish(rc, g[12], "sgmv_rms_norm_q8");
+}
+
+static PyObject* call_silu_mul(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"dtype", "out", "q", "q_scales", "gate", "up", "n_tokens", "h", "stream", "check"};
+  PyObject* g[10];
+  void* a[5];  // out .. up
+  void* stream;
+  int32_t dtype, n_tokens, h;
+  int rc = sort_arguments(names, 10, 8, args, nargs, kwnames, g);
+  FIRST(int32_of(g[0], &dtype));
+  for (int i = 0; i < 5; ++i) FIRST(address_of(g[1 + i], &a[i]));
+  FIRST(int32_of(g[6], &n_tokens));
+  FIRST(int32_of(g[7], &h));
+  FIRST(stream_of(g[8], &stream));
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[SILU_MUL], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_silu_mul(dtype, a[0], (int8_t*)a[1], (float*)a[2], a[3], a[4], n_tokens, h, stream);
+  Py_END_ALLOW_THREADS
+  return finish(rc, g[9], "sgmv_silu_mul_q8");
+}
+
+static PyObject* call_quantize(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"dtype", "q", "q_scales", "x", "n_tokens", "h", "stream", "check"};
+  PyObject* g[8];
+  void* a[3];  // q .. x
+  void* stream;
+  int32_t dtype, n_tokens, h;
+  int rc = sort_arguments(names, 8, 6, args, nargs, kwnames, g);
+  FIRST(int32_of(g[0], &dtype));
+  for (int i = 0; i < 3; ++i) FIRST(address_of(g[1 + i], &a[i]));
+  FIRST(int32_of(g[4], &n_tokens));
+  FIRST(int32_of(g[5], &h));
+  FIRST(stream_of(g[6], &stream));
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[QUANTIZE], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_quantize(dtype, (int8_t*)a[0], (float*)a[1], a[2], n_tokens, h, stream);
+  Py_END_ALLOW_THREADS
+  return finish(rc, g[7], "sgmv_quantize_q8");
+}
+
+// A list's or tuple's `n` whole numbers (an element's __index__ is Python code too).
+static int widths_of(PyObject* seq, Py_ssize_t n, int32_t* out) {
+  if (!(PyList_Check(seq) || PyTuple_Check(seq)) || PySequence_Fast_GET_SIZE(seq) != n) return UNUSUAL;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    out[i] = 0;
+    if (i >= PySequence_Fast_GET_SIZE(seq)) continue;
+    PyObject* element = PySequence_Fast_GET_ITEM(seq, i);
+    Py_INCREF(element);
+    const int rc = int32_of(element, &out[i]);
+    Py_DECREF(element);
+    if (rc != DONE) return rc;
+  }
+  return DONE;
+}
+
+static int size_of(PyObject* o, size_t* out) {
+  if (o == NULL) {
+    *out = 0;
+    return DONE;
+  }
+  if (!PyLong_Check(o)) return UNUSUAL;
+  *out = PyLong_AsSize_t(o);
+  return *out == (size_t)-1 && PyErr_Occurred() ? unusual() : DONE;
+}
+
+static PyObject* call_dense(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"dtype",    "ys",   "q",      "q_scales",  "ws",              "w_scales",
+                                      "n_tokens", "h_in", "h_outs", "workspace", "workspace_bytes", "stream", "check"};
+  PyObject* g[13];
+  void *ys[MOST_ADD_ONS], *ws[MOST_ADD_ONS], *scales[MOST_ADD_ONS], *q, *q_scales, *workspace, *stream;
+  int32_t dtype, n_tokens, h_in, h_outs[MOST_ADD_ONS];
+  size_t bytes;
+  Py_ssize_t n = 0;
+  int rc = sort_arguments(names, 13, 9, args, nargs, kwnames, g);
+  if (rc == DONE) {
+    n = PyList_Check(g[1]) || PyTuple_Check(g[1]) ? PySequence_Fast_GET_SIZE(g[1]) : MOST_ADD_ONS + 1;
+    if (n > MOST_ADD_ONS) rc = UNUSUAL;
+  }
+  FIRST(int32_of(g[0], &dtype));
+  FIRST(addresses_of(g[1], n, ys));
+  FIRST(address_of(g[2], &q));
+  FIRST(address_of(g[3], &q_scales));
+  FIRST(addresses_of(g[4], n, ws));
+  FIRST(addresses_of(g[5], n, scales));
+  FIRST(int32_of(g[6], &n_tokens));
+  FIRST(int32_of(g[7], &h_in));
+  FIRST(widths_of(g[8], n, h_outs));
+  FIRST(address_of(g[9] == NULL ? Py_None : g[9], &workspace));
+  FIRST(size_of(g[10], &bytes));
+  FIRST(stream_of(g[11], &stream));
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[DENSE], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_dense(dtype, (int32_t)n, ys, (const int8_t*)q, (const float*)q_scales, (const int8_t* const*)ws,
+                (const float* const*)scales, n_tokens, h_in, h_outs, workspace, bytes, stream);
+  Py_END_ALLOW_THREADS
+  return finish(rc, g[12], "sgmv_dense_q8");
+}
+
+// bind(problem type, error type, then of the calls, in the order of the enumeration above, the
+// addresses and the functions in Python)
 static PyObject* call_bind(PyObject* self, PyObject* args) {
-  PyObject *problem, *error, *g[5];
-  unsigned long long f[5];
-  if (!PyArg_ParseTuple(args, "OO(KKKKK)(OOOOO)", &problem, &error, &f[0], &f[1], &f[2], &f[3], &f[4], &g[0], &g[1], &g[2],
-                        &g[3], &g[4]))
+  PyObject *problem, *error, *addresses, *functions;
+  if (!PyArg_ParseTuple(args, "OOO!O!", &problem, &error, &PyTuple_Type, &addresses, &PyTuple_Type, &functions)) return NULL;
+  if (PyTuple_GET_SIZE(addresses) != CALLS || PyTuple_GET_SIZE(functions) != CALLS) {
+    PyErr_SetString(PyExc_ValueError, "an address and a function for every call");
     return NULL;
+  }
+  unsigned long long f[CALLS];
+  for (int i = 0; i < CALLS; ++i) {
+    f[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i));
+    if (f[i] == (unsigned long long)-1 && PyErr_Occurred()) return NULL;
+  }
   Py_INCREF(problem);
   Py_INCREF(error);
   Py_XSETREF(problem_type, problem);
   Py_XSETREF(error_type, error);
-  for (int i = 0; i < 5; ++i) {
-    Py_INCREF(g[i]);
-    Py_XSETREF(general[i], g[i]);
+  for (int i = 0; i < CALLS; ++i) {
+    PyObject* function = PyTuple_GET_ITEM(functions, i);
+    Py_INCREF(function);
+    Py_XSETREF(general[i], function);
   }
   fn_shrink = (shrink_fn)(uintptr_t)f[SHRINK];
   fn_expand = (expand_fn)(uintptr_t)f[EXPAND];
   fn_add_lora = (add_lora_fn)(uintptr_t)f[ADD_LORA];
   fn_add_lora_static = (add_lora_fn)(uintptr_t)f[ADD_LORA_STATIC];
   fn_add_lora_multi = (add_lora_multi_fn)(uintptr_t)f[ADD_LORA_MULTI];
+  fn_rms_norm = (rms_norm_fn)(uintptr_t)f[RMS_NORM];
+  fn_silu_mul = (silu_mul_fn)(uintptr_t)f[SILU_MUL];
+  fn_quantize = (quantize_fn)(uintptr_t)f[QUANTIZE];
+  fn_dense = (dense_fn)(uintptr_t)f[DENSE];
   return PyLong_FromSize_t(sizeof(sgmv_problem));
 }
 
@@ -320,6 +459,15 @@ static PyMethodDef methods[] = {
     FAST("sgmv_add_lora_multi", call_add_lora_multi,
          "sgmv_add_lora_multi(p, ys, xs, A_ptrs, B_ptrs, seg_starts, n_segs, layer_idx, scale, stream=None, check=True)\n"
          "--\n\nys, xs, A_ptrs, B_ptrs are sequences of equal length (one entry per add-on)."),
+    FAST("sgmv_rms_norm_q8", call_rms_norm,
+         "sgmv_rms_norm_q8(dtype, out, q, q_scales, sum, x, residual, weight, eps, n_tokens, h, stream=None, check=True)\n--\n\n"),
+    FAST("sgmv_silu_mul_q8", call_silu_mul,
+         "sgmv_silu_mul_q8(dtype, out, q, q_scales, gate, up, n_tokens, h, stream=None, check=True)\n--\n\n"),
+    FAST("sgmv_quantize_q8", call_quantize,
+         "sgmv_quantize_q8(dtype, q, q_scales, x, n_tokens, h, stream=None, check=True)\n--\n\n"),
+    FAST("sgmv_dense_q8", call_dense,
+         "sgmv_dense_q8(dtype, ys, q, q_scales, ws, w_scales, n_tokens, h_in, h_outs, workspace=None, workspace_bytes=0, "
+         "stream=None, check=True)\n--\n\nys, ws, w_scales, h_outs are sequences of equal length (one entry per projection)."),
     {"bind", call_bind, METH_VARARGS, "bind(problem_type, error_type, addresses, functions) -> size of the C struct"},
     {NULL, NULL, 0, NULL}};
 

@@ -1,0 +1,47 @@
+// Host-side launch descriptors of the 8-bit backbone kernels (q8_rows.hip, q8_dense.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace sgmv {
+
+// Widest row that one workgroup of the row kernels holds in registers: 1024 threads, four chunks of eight values each.
+constexpr int kRowsMostWidth = 1024 * 4 * 8;
+// Widest input of a dense projection: 128 * 128 * h_in stays below 2^31.
+constexpr int kDenseMostHin = 131064;
+// Most projections of one sgmv_dense_q8 call.
+constexpr int kDenseMostProjections = 8;
+
+enum RowsKind { kRowsNorm, kRowsSiluMul, kRowsQuantize };
+
+struct RowsArgs {
+  RowsKind kind;
+  bool bf16;
+  int n_tokens, h;
+  float eps;
+  const void* x;         // rows; the gate of kRowsSiluMul
+  const void* other;     // residual of kRowsNorm (may be nullptr), up of kRowsSiluMul
+  const void* weight;    // kRowsNorm
+  void* sum;             // kRowsNorm, may be nullptr
+  void* out;             // 16-bit result, may be nullptr
+  int8_t* q;             // 8-bit result with its scales, both or neither
+  float* q_scales;
+};
+hipError_t launch_rows(const RowsArgs& a, hipStream_t st);
+
+struct DenseArgs {
+  bool bf16;
+  int n_tokens, h_in, n_proj;
+  const int8_t* q;
+  const float* q_scales;
+  int h_out[kDenseMostProjections];
+  const int8_t* w[kDenseMostProjections];
+  const float* w_scales[kDenseMostProjections];
+  void* y[kDenseMostProjections];
+  void* workspace;       // may be nullptr
+  size_t workspace_bytes;
+};
+hipError_t launch_dense(const DenseArgs& a, hipStream_t st);
+
+}  // namespace sgmv

@@ -1,0 +1,110 @@
+// C ABI of the 8-bit backbone: argument checks and dispatch (include/sgmv.h, last section).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/sgmv.h"
+#include "q8.h"
+
+namespace {
+
+using namespace sgmv;
+
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+int check_rows(int32_t dtype, int32_t n_tokens, int32_t h) {
+  if (dtype != SGMV_F16 && dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
+  if (n_tokens < 0 || h <= 0) return SGMV_ERR_SHAPE;
+  if (h % 8 != 0 || h > kRowsMostWidth) return SGMV_ERR_UNSUPPORTED;
+  return SGMV_OK;
+}
+
+// The two parts of an 8-bit result go together; `must`: they cannot be left out.
+int check_q8(const int8_t* q, const float* q_scales, bool must) {
+  if ((q == nullptr) != (q_scales == nullptr) || (must && q == nullptr)) return SGMV_ERR_NULL;
+  if (!aligned(q, 16) || !aligned(q_scales, 4)) return SGMV_ERR_ALIGN;
+  return SGMV_OK;
+}
+
+int launch(const RowsArgs& a, void* stream) {
+  return launch_rows(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sgmv_rms_norm_q8(int32_t dtype, void* out, int8_t* q, float* q_scales, void* sum, const void* x, const void* residual,
+                     const void* weight, float eps, int32_t n_tokens, int32_t h, void* stream) {
+  int rc = check_rows(dtype, n_tokens, h);
+  if (rc != SGMV_OK) return rc;
+  if (!(eps >= 0.0f) || !(eps < __builtin_inff())) return SGMV_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return SGMV_OK;
+  if (x == nullptr || weight == nullptr || (out == nullptr && q == nullptr)) return SGMV_ERR_NULL;
+  rc = check_q8(q, q_scales, false);
+  if (rc != SGMV_OK) return rc;
+  if (!aligned(out, 16) || !aligned(sum, 16) || !aligned(x, 16) || !aligned(residual, 16) || !aligned(weight, 16)) return SGMV_ERR_ALIGN;
+  if (out != nullptr && (out == sum || out == weight)) return SGMV_ERR_SHAPE;
+  return launch(RowsArgs{kRowsNorm, dtype == SGMV_BF16, n_tokens, h, eps, x, residual, weight, sum, out, q, q_scales}, stream);
+}
+
+int sgmv_silu_mul_q8(int32_t dtype, void* out, int8_t* q, float* q_scales, const void* gate, const void* up, int32_t n_tokens,
+                     int32_t h, void* stream) {
+  int rc = check_rows(dtype, n_tokens, h);
+  if (rc != SGMV_OK) return rc;
+  if (n_tokens == 0) return SGMV_OK;
+  if (gate == nullptr || up == nullptr || (out == nullptr && q == nullptr)) return SGMV_ERR_NULL;
+  rc = check_q8(q, q_scales, false);
+  if (rc != SGMV_OK) return rc;
+  if (!aligned(out, 16) || !aligned(gate, 16) || !aligned(up, 16)) return SGMV_ERR_ALIGN;
+  return launch(RowsArgs{kRowsSiluMul, dtype == SGMV_BF16, n_tokens, h, 0.0f, gate, up, nullptr, nullptr, out, q, q_scales}, stream);
+}
+
+int sgmv_quantize_q8(int32_t dtype, int8_t* q, float* q_scales, const void* x, int32_t n_tokens, int32_t h, void* stream) {
+  int rc = check_rows(dtype, n_tokens, h);
+  if (rc != SGMV_OK) return rc;
+  if (n_tokens == 0) return SGMV_OK;
+  if (x == nullptr) return SGMV_ERR_NULL;
+  rc = check_q8(q, q_scales, true);
+  if (rc != SGMV_OK) return rc;
+  if (!aligned(x, 16)) return SGMV_ERR_ALIGN;
+  return launch(RowsArgs{kRowsQuantize, dtype == SGMV_BF16, n_tokens, h, 0.0f, x, nullptr, nullptr, nullptr, nullptr, q, q_scales}, stream);
+}
+
+int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* q, const float* q_scales, const int8_t* const* ws,
+                  const float* const* w_scales, int32_t n_tokens, int32_t h_in, const int32_t* h_outs, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+  if (dtype != SGMV_F16 && dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
+  if (n_proj < 0 || n_proj > kDenseMostProjections || n_tokens < 0 || h_in <= 0) return SGMV_ERR_SHAPE;
+  if (h_in % 8 != 0 || h_in > kDenseMostHin) return SGMV_ERR_UNSUPPORTED;
+  if (n_proj == 0) return SGMV_OK;
+  if (h_outs == nullptr) return SGMV_ERR_NULL;
+  for (int i = 0; i < n_proj; ++i) {
+    if (h_outs[i] <= 0) return SGMV_ERR_SHAPE;
+    if (h_outs[i] % 8 != 0) return SGMV_ERR_UNSUPPORTED;
+  }
+  if (n_tokens == 0) return SGMV_OK;
+  if (ys == nullptr || q == nullptr || q_scales == nullptr || ws == nullptr || w_scales == nullptr) return SGMV_ERR_NULL;
+  if (!aligned(q, 16) || !aligned(q_scales, 4) || !aligned(workspace, 256)) return SGMV_ERR_ALIGN;
+  DenseArgs a = {};
+  a.bf16 = dtype == SGMV_BF16;
+  a.n_tokens = n_tokens;
+  a.h_in = h_in;
+  a.n_proj = n_proj;
+  a.q = q;
+  a.q_scales = q_scales;
+  a.workspace = workspace;
+  a.workspace_bytes = workspace == nullptr ? 0 : workspace_bytes;
+  for (int i = 0; i < n_proj; ++i) {
+    if (ys[i] == nullptr || ws[i] == nullptr || w_scales[i] == nullptr) return SGMV_ERR_NULL;
+    if (!aligned(ys[i], 16) || !aligned(ws[i], 16) || !aligned(w_scales[i], 16)) return SGMV_ERR_ALIGN;
+    for (int j = 0; j < i; ++j)
+      if (ys[i] == ys[j]) return SGMV_ERR_SHAPE;  // two projections into one y would race
+    a.h_out[i] = h_outs[i];
+    a.w[i] = ws[i];
+    a.w_scales[i] = w_scales[i];
+    a.y[i] = ys[i];
+  }
+  return launch_dense(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,184 @@
+// Row kernels of the 8-bit backbone (gfx950): rms norm with the residual's addition, silu(gate) * up, and plain rows,
+// each with an 8-bit output and a scale per row, the first two with a 16-bit output as well.
+//
+//   norm      s = x + residual;  v = s * rsqrt(mean(s^2) + eps) * weight
+//   silu      v = gate / (1 + exp(-gate)) * up
+//   quantize  v = x
+//   8 bits    top = max |v|;  scale = top / 127;  q = v * (127 / top), rounded to the nearest even
+//
+// All of it is fp32 between the 16-bit loads and the stores.  In the norm the factor rsqrt(...) is common to the
+// row and cancels in q, so the row's maximum is taken of |s * weight| and one reduction of two numbers serves both:
+// a row is read once, kept in registers, reduced once and written.
+//
+// The maximum is taken of the bit patterns of |v| as unsigned integers, which puts infinities above every number and NaN
+// above those: one comparison against the infinity's pattern tells a row that holds something not finite.
+#include "device_common.h"
+#include "q8.h"
+
+namespace sgmv {
+
+namespace {
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// Sum and maximum over the workgroup, in every thread.
+__device__ __forceinline__ void reduce_row(float& sum, uint32_t& top, float* sums, uint32_t* tops) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    sum += __shfl_xor(sum, m);
+    const uint32_t t = __shfl_xor(top, m);
+    top = t > top ? t : top;
+  }
+  const int waves = blockDim.x >> 6;
+  if (waves == 1) return;
+  if ((threadIdx.x & 63) == 0) {
+    sums[threadIdx.x >> 6] = sum;
+    tops[threadIdx.x >> 6] = top;
+  }
+  __syncthreads();
+  sum = 0.0f;
+  top = 0;
+  for (int w = 0; w < waves; ++w) {
+    sum += sums[w];
+    top = tops[w] > top ? tops[w] : top;
+  }
+}
+
+// One workgroup per row, CHUNKS pieces of eight values to a thread.  grid = rows.
+template <class DT, RowsKind KIND, int CHUNKS>
+__global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* __restrict__ x, const uint16_t* other,
+                                                       const uint16_t* __restrict__ weight, uint16_t* sum_out, uint16_t* out,
+                                                       int8_t* q, float* q_scales, int h, float eps) {
+  __shared__ float sums[2][16];
+  __shared__ uint32_t tops[2][16];
+  const size_t base = (size_t)blockIdx.x * (size_t)h;
+  float v[CHUNKS][8];  // norm: s; else the values themselves
+  float w[KIND == kRowsNorm ? CHUNKS : 1][8];
+  float sum = 0.0f;
+  uint32_t top = 0;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int at = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+    uint4 a = make_uint4(0, 0, 0, 0), b = a, g = a;
+    if (at < h) {
+      a = load128(x + base + at);
+      if (KIND == kRowsSiluMul || (KIND == kRowsNorm && other != nullptr)) b = load128(other + base + at);
+      if (KIND == kRowsNorm) g = load128(weight + at);
+    }
+    unpack8<DT>(a, v[c]);
+    float t[8];
+    unpack8<DT>(b, t);
+    if constexpr (KIND == kRowsNorm) {
+      unpack8<DT>(g, w[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] += t[i];  // without a residual: + 0
+    } else if constexpr (KIND == kRowsSiluMul) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // (1 + exp(-gate)) / 256: the reciprocal instruction gives zero for results under 2^-126, that of 1 + exp(88) is one
+        const float d = fmaf(__expf(-v[c][i]), 0x1p-8f, 0x1p-8f);
+        v[c][i] = __builtin_amdgcn_rcpf(d) * 0x1p-8f * v[c][i] * t[i];
+      }
+    }
+    if (KIND == kRowsNorm && sum_out != nullptr && at < h)
+      store128(sum_out + base + at, make_uint4(pack2<DT>(v[c][0], v[c][1]), pack2<DT>(v[c][2], v[c][3]), pack2<DT>(v[c][4], v[c][5]),
+                                               pack2<DT>(v[c][6], v[c][7])));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (KIND == kRowsNorm) sum += v[c][i] * v[c][i];
+      const float p = KIND == kRowsNorm ? v[c][i] * w[KIND == kRowsNorm ? c : 0][i] : v[c][i];
+      const uint32_t bits = __float_as_uint(p) & 0x7FFFFFFFu;
+      top = bits > top ? bits : top;
+    }
+  }
+  reduce_row(sum, top, sums[0], tops[0]);
+  float inv = 1.0f;
+  if constexpr (KIND == kRowsNorm) {
+    if ((__float_as_uint(sum) & 0x7FFFFFFFu) >= kInfBits) {
+      // values past about 1e18, whose squares leave fp32's range: the row times 2^-80, which the norm does not change by
+      // (what is not finite itself stays so)
+      constexpr float kDown = 0x1p-80f;
+      sum = 0.0f;
+      top = 0;
+      eps = eps * kDown * kDown;
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v[c][i] *= kDown;
+          sum += v[c][i] * v[c][i];
+          const uint32_t bits = __float_as_uint(v[c][i] * w[c][i]) & 0x7FFFFFFFu;
+          top = bits > top ? bits : top;
+        }
+      reduce_row(sum, top, sums[1], tops[1]);
+    }
+    inv = 1.0f / sqrtf(sum / (float)h + eps);
+  }
+  const bool finite = top < kInfBits && __float_as_uint(inv) < kInfBits;
+  float peak = __uint_as_float(top);
+  if (q_scales != nullptr && threadIdx.x == 0)
+    q_scales[blockIdx.x] = finite ? inv * peak / 127.0f : __uint_as_float(0x7FC00000u);
+  // 127 / peak leaves fp32's range for the smallest peaks: those rows are made larger first
+  const float up = peak < 0x1p-60f ? 0x1p64f : 1.0f;
+  const float factor = finite && top != 0 ? 127.0f / (peak * up) : 0.0f;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int at = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+    if (at >= h) break;
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = KIND == kRowsNorm ? v[c][i] * inv * w[KIND == kRowsNorm ? c : 0][i] : v[c][i];
+    if (KIND != kRowsQuantize && out != nullptr)
+      store128(out + base + at, make_uint4(pack2<DT>(r[0], r[1]), pack2<DT>(r[2], r[3]), pack2<DT>(r[4], r[5]), pack2<DT>(r[6], r[7])));
+    if (q != nullptr) {
+      uint32_t packed[2] = {0, 0};
+      if (finite) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float p = KIND == kRowsNorm ? v[c][i] * w[KIND == kRowsNorm ? c : 0][i] : v[c][i];
+          packed[i >> 2] |= ((uint32_t)(int)rintf(p * up * factor) & 0xFFu) << (8 * (i & 3));
+        }
+      }
+      *reinterpret_cast<uint2*>(q + base + at) = make_uint2(packed[0], packed[1]);
+    }
+  }
+}
+
+template <class DT, RowsKind KIND>
+hipError_t launch_kind(const RowsArgs& a, hipStream_t st) {
+  // threads of a row: few rows want a row's loads spread over as many lanes as it has pieces, many rows fewer, fuller waves
+  const int pieces = a.h / 8;
+  int chunks = a.n_tokens >= 512 ? 4 : 1;
+  while (chunks < 4 && pieces > 1024 * chunks) chunks *= 2;
+  while (chunks > 1 && pieces <= 64 * (chunks / 2)) chunks /= 2;
+  const int threads = ((pieces + chunks - 1) / chunks + 63) / 64 * 64;
+  const dim3 grid((unsigned)a.n_tokens), block((unsigned)threads);
+  auto launch = [&](auto kernel) {
+    kernel<<<grid, block, 0, st>>>(static_cast<const uint16_t*>(a.x), static_cast<const uint16_t*>(a.other),
+                                   static_cast<const uint16_t*>(a.weight), static_cast<uint16_t*>(a.sum),
+                                   static_cast<uint16_t*>(a.out), a.q, a.q_scales, a.h, a.eps);
+  };
+  switch (chunks) {
+    case 1: launch(rows_q8_kernel<DT, KIND, 1>); break;
+    case 2: launch(rows_q8_kernel<DT, KIND, 2>); break;
+    default: launch(rows_q8_kernel<DT, KIND, 4>); break;
+  }
+  return hipGetLastError();
+}
+
+template <class DT>
+hipError_t launch_typed(const RowsArgs& a, hipStream_t st) {
+  switch (a.kind) {
+    case kRowsNorm: return launch_kind<DT, kRowsNorm>(a, st);
+    case kRowsSiluMul: return launch_kind<DT, kRowsSiluMul>(a, st);
+    default: return launch_kind<DT, kRowsQuantize>(a, st);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rows(const RowsArgs& a, hipStream_t st) {
+  return a.bf16 ? launch_typed<BF16>(a, st) : launch_typed<F16>(a, st);
+}
+
+}  // namespace sgmv
