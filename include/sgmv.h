@@ -163,7 +163,11 @@ typedef enum {
   SGMV_KERNEL_VECTOR = 5,           /* one launch per step, vector ALUs                    */
   SGMV_KERNEL_MATRIX = 6,           /* one launch per step, MFMA (long segments)           */
   SGMV_KERNEL_SEQUENCE = 7,         /* internal: multi-projection call run as single calls */
-  SGMV_KERNEL_WHOLE = 8             /* single launch, whole shrink in every workgroup      */
+  SGMV_KERNEL_WHOLE = 8,            /* single launch, whole shrink in every workgroup      */
+  SGMV_KERNEL_DENSE_FEW = 9,        /* sgmv_dense_q8: few tokens, a workgroup's waves      */
+                                    /* divide h_in                                         */
+  SGMV_KERNEL_DENSE_SMALL = 10,     /* ... tiles of up to 128 x 128                        */
+  SGMV_KERNEL_DENSE_LARGE = 11      /* ... tiles of up to 256 x 256                        */
 } sgmv_kernel;
 
 /* What a call would launch: plain data filled by sgmv_plan_add_lora. */
@@ -410,20 +414,25 @@ int sgmv_quantize_q8(int32_t dtype, int8_t* q, float* q_scales, const void* x, i
  * The sum is an exact 32-bit integer, scaled in fp32 and rounded once when y is stored (y is
  * written, not accumulated into).
  *   ys        HOST array of device pointers, y_i 16-bit [n_tokens][h_outs[i]], distinct
- *   q, q_scales  device, as above, width h_in, at most 131064 (else SGMV_ERR_UNSUPPORTED); any int8
- *             values (-128 too)
+ *   q, q_scales  device, as above, width h_in, at most 131064; any int8 values (-128 too)
  *   ws        HOST array of device pointers, w_i int8 [h_outs[i]][h_in] (an output channel's weights
  *             in a row)
  *   w_scales  HOST array of device pointers, fp32 [h_outs[i]]
- *   h_outs    HOST array of output widths
+ *   h_outs    HOST array of output widths, at most 2^27 (n_tokens at most 2^30; else SGMV_ERR_UNSUPPORTED)
  *   workspace device scratch, 256-byte aligned, or NULL with 0 bytes.  Shapes with few output tiles
- *             and a long h_in divide the sum over more workgroups where their partial sums fit in it;
- *             SGMV_DENSE_WORKSPACE_BYTES is enough for every shape.  It needs no preparation, keeps
- *             nothing between calls, and calls that share it must be ordered. */
+ *             and a long h_in divide the sum over more workgroups where their partial sums (4 bytes for
+ *             every value of y and part) fit in it; SGMV_DENSE_WORKSPACE_BYTES is enough for nearly all
+ *             that gain by it.  It needs no preparation, keeps nothing between calls, and calls that
+ *             share it must be ordered.  The result is the same to the bit with any workspace. */
 #define SGMV_DENSE_WORKSPACE_BYTES ((size_t)16 << 20)
 int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* q, const float* q_scales,
                   const int8_t* const* ws, const float* const* w_scales, int32_t n_tokens, int32_t h_in,
                   const int32_t* h_outs, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Host-only, pure: which kernel sgmv_dense_q8 would launch (`slices` = parts of the sum; with more than
+ * one a second launch joins them).  Returns the status that the call's sizes alone give. */
+int sgmv_plan_dense_q8(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, const int32_t* h_outs,
+                       const void* workspace, size_t workspace_bytes, sgmv_plan* plan);
 
 /* Measurement aid, not part of the operator: enqueue one plain kernel of known traffic on
  * `stream`, for the benchmark's attainable-bandwidth figure and for scaling a profiler's HBM

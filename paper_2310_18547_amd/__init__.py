@@ -13,7 +13,8 @@ _BINDING_NAMES = (
     "sgmv_status_string", "sgmv_validate_segments", "sgmv_workspace_bytes", "sgmv_workspace_init",
     "sgmv_workspace_check", "sgmv_probe", "PROBE_EMPTY", "PROBE_READ", "PROBE_COPY", "PROBE_HANDOFF",
     "STATIC_SCRATCH_BYTES", "STATIC_MAX_WORKSPACE_BYTES",
-    "sgmv_rms_norm_q8", "sgmv_silu_mul_q8", "sgmv_quantize_q8", "sgmv_dense_q8", "DENSE_WORKSPACE_BYTES",
+    "sgmv_rms_norm_q8", "sgmv_silu_mul_q8", "sgmv_quantize_q8", "sgmv_dense_q8", "sgmv_plan_dense_q8", "DENSE_WORKSPACE_BYTES",
+    "KERNEL_DENSE_FEW", "KERNEL_DENSE_SMALL", "KERNEL_DENSE_LARGE",
 )
 __all__ = list(_BINDING_NAMES)
 

@@ -63,10 +63,11 @@ class SgmvPlan(ctypes.Structure):
 
 
 KERNEL_NONE, KERNEL_FUSED, KERNEL_TILE, KERNEL_MULTI_SIDE, KERNEL_MULTI_PIPELINED, KERNEL_VECTOR, \
-    KERNEL_MATRIX, KERNEL_SEQUENCE, KERNEL_WHOLE = range(9)
+    KERNEL_MATRIX, KERNEL_SEQUENCE, KERNEL_WHOLE, KERNEL_DENSE_FEW, KERNEL_DENSE_SMALL, KERNEL_DENSE_LARGE = range(12)
 KERNEL_NAMES = {KERNEL_NONE: "none", KERNEL_FUSED: "fused", KERNEL_TILE: "tile",
                 KERNEL_MULTI_SIDE: "multi_side", KERNEL_MULTI_PIPELINED: "multi_pipelined",
-                KERNEL_VECTOR: "vector", KERNEL_MATRIX: "matrix", KERNEL_WHOLE: "whole"}
+                KERNEL_VECTOR: "vector", KERNEL_MATRIX: "matrix", KERNEL_WHOLE: "whole", KERNEL_DENSE_FEW: "dense_few",
+                KERNEL_DENSE_SMALL: "dense_small", KERNEL_DENSE_LARGE: "dense_large"}
 
 
 def _load():
@@ -114,6 +115,9 @@ def _load():
     L.sgmv_dense_q8.argtypes = [c.c_int32, c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
                                 c.c_int32, c.c_int32, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
     L.sgmv_dense_q8.restype = c.c_int
+    L.sgmv_plan_dense_q8.argtypes = [c.c_int32, c.c_int32, c.c_int32, c.c_int32, c.c_void_p, c.c_void_p, c.c_size_t,
+                                     c.POINTER(SgmvPlan)]
+    L.sgmv_plan_dense_q8.restype = c.c_int
     L.sgmv_probe.argtypes = [c.c_int, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
     L.sgmv_probe.restype = c.c_int
     L.sgmv_plan_add_lora.argtypes = [P, c.c_int32, c.c_int32, c.POINTER(SgmvPlan)]
@@ -301,6 +305,18 @@ def sgmv_plan_shrink(p: SgmvProblem, n_segs: int, check: bool = True):
         return rc, plan
     if rc != 0:
         raise SgmvError(rc, "sgmv_plan_shrink")
+    return plan
+
+
+def sgmv_plan_dense_q8(dtype: int, n_tokens: int, h_in: int, h_outs, workspace=None, workspace_bytes: int = 0, check: bool = True):
+    """Host-only: the ``SgmvPlan`` of a ``sgmv_dense_q8`` call (``check=False``: ``(status, plan)``)."""
+    plan = SgmvPlan()
+    rc = lib.sgmv_plan_dense_q8(dtype, len(h_outs), n_tokens, h_in, (ctypes.c_int32 * len(h_outs))(*h_outs), _addr(workspace),
+                                workspace_bytes, ctypes.byref(plan))
+    if not check:
+        return rc, plan
+    if rc != 0:
+        raise SgmvError(rc, "sgmv_plan_dense_q8")
     return plan
 
 

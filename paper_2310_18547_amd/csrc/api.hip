@@ -24,6 +24,26 @@ constexpr size_t kStaticBytes = (size_t)9 << 20;
 static __device__ __align__(256) unsigned char scratch[kStaticBytes];
 static_assert(kStaticBytes == SGMV_STATIC_SCRATCH_BYTES, "the header states the array's size");
 
+int sgmv::compute_units() {
+  constexpr int kMaxDevices = 64;
+  constexpr int kDefaultComputeUnits = 256;  // MI355X; assumed where no device can be asked
+  static std::atomic<int> cached[kMaxDevices];  // zero-initialised
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
+    (void)hipGetLastError();  // no device here (a host-only query): leave no sticky error behind
+    return kDefaultComputeUnits;
+  }
+  int cu = cached[dev].load(std::memory_order_relaxed);
+  if (cu == 0) {
+    if (hipDeviceGetAttribute(&cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cu <= 0) {
+      (void)hipGetLastError();
+      cu = kDefaultComputeUnits;
+    }
+    cached[dev].store(cu, std::memory_order_relaxed);
+  }
+  return cu;
+}
+
 namespace {
 
 using namespace sgmv;
@@ -42,7 +62,6 @@ constexpr int kTileMultiSlices = 4;    // fewest slices at which a joint tile la
 constexpr int kFusedMaxWorkgroups = kGenerationCopies;  // every workgroup of a launch has its own generation copy
 constexpr int kFusedSpinLimit = 1 << 18;
 constexpr int kMaxDevices = 64;
-constexpr int kDefaultComputeUnits = 256;  // MI355X; assumed where no device can be asked
 
 // Residency limits of the single-launch kernels.  They follow from the compute units of the
 // current device (asked once per device): a workgroup that waits for the partial sums of a
@@ -54,24 +73,6 @@ struct Limits {
   int multi_workgroups;       // multi-projection launch side by side (two per unit)
   int multi_workgroups_most;  // ... where the pipelined kernel does not apply (three per unit)
 };
-
-int compute_units() {
-  static std::atomic<int> cached[kMaxDevices];  // zero-initialised
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
-    (void)hipGetLastError();  // no device here (a host-only query): leave no sticky error behind
-    return kDefaultComputeUnits;
-  }
-  int cu = cached[dev].load(std::memory_order_relaxed);
-  if (cu == 0) {
-    if (hipDeviceGetAttribute(&cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cu <= 0) {
-      (void)hipGetLastError();
-      cu = kDefaultComputeUnits;
-    }
-    cached[dev].store(cu, std::memory_order_relaxed);
-  }
-  return cu;
-}
 
 Limits limits() {
   const int cu = compute_units();

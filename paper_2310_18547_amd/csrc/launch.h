@@ -181,6 +181,8 @@ inline bool stream_weights(bool by_rows, int n_tokens, int n_segs, int r, long l
 // Items of a per-row launch that takes two rows of a segment to an item (device_common.h, find_rows); some stay empty.
 __host__ __device__ inline int pair_places(int n_tokens, int n_segs) { return (n_tokens + n_segs) / 2; }
 
+// Compute units of the current device (asked once per device); those of an MI355X where there is none.
+int compute_units();
 size_t tile_lds_bytes(int r, int kslice, int cslice);
 hipError_t launch_add_lora_whole(const WholeArgs& a, hipStream_t st);
 hipError_t launch_add_lora_tile(const TileArgs& a, hipStream_t st);

@@ -10,6 +10,8 @@ namespace sgmv {
 constexpr int kRowsMostWidth = 1024 * 4 * 8;
 // Widest input of a dense projection: 128 * 128 * h_in stays below 2^31.
 constexpr int kDenseMostHin = 131064;
+// Most tokens, and widest output of a projection: rows and channels, all projections' together, are 32-bit numbers.
+constexpr int kDenseMostTokens = 1 << 30, kDenseMostHout = 1 << 27;
 // Most projections of one sgmv_dense_q8 call.
 constexpr int kDenseMostProjections = 8;
 
@@ -42,6 +44,16 @@ struct DenseArgs {
   void* workspace;       // may be nullptr
   size_t workspace_bytes;
 };
-hipError_t launch_dense(const DenseArgs& a, hipStream_t st);
+enum DenseFamily { kDenseFew, kDenseSmall, kDenseLarge };
+struct DensePlan {
+  int kernel;            // of q8_dense.hip's table
+  DenseFamily family;
+  int splits;            // workgroups that divide a tile's sum; from two on a second launch joins the parts
+  long long workgroups;
+  int lds;               // bytes per workgroup
+};
+// The kernel for a call on a device of that many compute units; pure host arithmetic.  False: no launch takes it.
+bool plan_dense(const DenseArgs& a, int units, DensePlan* plan);
+hipError_t launch_dense(const DenseArgs& a, const DensePlan& plan, hipStream_t st);
 
 }  // namespace sgmv

@@ -3,6 +3,7 @@
 #include <stdint.h>
 
 #include "../../include/sgmv.h"
+#include "launch.h"
 #include "q8.h"
 
 namespace {
@@ -23,6 +24,34 @@ int check_q8(const int8_t* q, const float* q_scales, bool must) {
   if ((q == nullptr) != (q_scales == nullptr) || (must && q == nullptr)) return SGMV_ERR_NULL;
   if (!aligned(q, 16) || !aligned(q_scales, 4)) return SGMV_ERR_ALIGN;
   return SGMV_OK;
+}
+
+// What a dense call and its plan refuse alike; `*nothing`: the call has nothing to do.
+int check_dense(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, const int32_t* h_outs, const void* workspace,
+                bool* nothing) {
+  *nothing = n_proj == 0 || n_tokens == 0;
+  if (dtype != SGMV_F16 && dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
+  if (n_proj < 0 || n_proj > kDenseMostProjections || n_tokens < 0 || h_in <= 0) return SGMV_ERR_SHAPE;
+  if (h_in % 8 != 0 || h_in > kDenseMostHin || n_tokens > kDenseMostTokens) return SGMV_ERR_UNSUPPORTED;
+  if (n_proj > 0 && h_outs == nullptr) return SGMV_ERR_NULL;
+  for (int i = 0; i < n_proj; ++i) {
+    if (h_outs[i] <= 0) return SGMV_ERR_SHAPE;
+    if (h_outs[i] % 8 != 0 || h_outs[i] > kDenseMostHout) return SGMV_ERR_UNSUPPORTED;
+  }
+  return aligned(workspace, 256) ? SGMV_OK : SGMV_ERR_ALIGN;
+}
+
+DenseArgs dense_shape(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, const int32_t* h_outs, void* workspace,
+                      size_t workspace_bytes) {
+  DenseArgs a = {};
+  a.bf16 = dtype == SGMV_BF16;
+  a.n_tokens = n_tokens;
+  a.h_in = h_in;
+  a.n_proj = n_proj;
+  for (int i = 0; i < n_proj; ++i) a.h_out[i] = h_outs[i];
+  a.workspace = workspace;
+  a.workspace_bytes = workspace == nullptr ? 0 : workspace_bytes;
+  return a;
 }
 
 int launch(const RowsArgs& a, void* stream) {
@@ -73,38 +102,44 @@ int sgmv_quantize_q8(int32_t dtype, int8_t* q, float* q_scales, const void* x, i
 int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* q, const float* q_scales, const int8_t* const* ws,
                   const float* const* w_scales, int32_t n_tokens, int32_t h_in, const int32_t* h_outs, void* workspace,
                   size_t workspace_bytes, void* stream) {
-  if (dtype != SGMV_F16 && dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
-  if (n_proj < 0 || n_proj > kDenseMostProjections || n_tokens < 0 || h_in <= 0) return SGMV_ERR_SHAPE;
-  if (h_in % 8 != 0 || h_in > kDenseMostHin) return SGMV_ERR_UNSUPPORTED;
-  if (n_proj == 0) return SGMV_OK;
-  if (h_outs == nullptr) return SGMV_ERR_NULL;
-  for (int i = 0; i < n_proj; ++i) {
-    if (h_outs[i] <= 0) return SGMV_ERR_SHAPE;
-    if (h_outs[i] % 8 != 0) return SGMV_ERR_UNSUPPORTED;
-  }
-  if (n_tokens == 0) return SGMV_OK;
+  bool nothing = false;
+  const int rc = check_dense(dtype, n_proj, n_tokens, h_in, h_outs, workspace, &nothing);
+  if (rc != SGMV_OK || nothing) return rc;
   if (ys == nullptr || q == nullptr || q_scales == nullptr || ws == nullptr || w_scales == nullptr) return SGMV_ERR_NULL;
-  if (!aligned(q, 16) || !aligned(q_scales, 4) || !aligned(workspace, 256)) return SGMV_ERR_ALIGN;
-  DenseArgs a = {};
-  a.bf16 = dtype == SGMV_BF16;
-  a.n_tokens = n_tokens;
-  a.h_in = h_in;
-  a.n_proj = n_proj;
+  if (!aligned(q, 16) || !aligned(q_scales, 4)) return SGMV_ERR_ALIGN;
+  DenseArgs a = dense_shape(dtype, n_proj, n_tokens, h_in, h_outs, workspace, workspace_bytes);
   a.q = q;
   a.q_scales = q_scales;
-  a.workspace = workspace;
-  a.workspace_bytes = workspace == nullptr ? 0 : workspace_bytes;
   for (int i = 0; i < n_proj; ++i) {
     if (ys[i] == nullptr || ws[i] == nullptr || w_scales[i] == nullptr) return SGMV_ERR_NULL;
     if (!aligned(ys[i], 16) || !aligned(ws[i], 16) || !aligned(w_scales[i], 16)) return SGMV_ERR_ALIGN;
     for (int j = 0; j < i; ++j)
       if (ys[i] == ys[j]) return SGMV_ERR_SHAPE;  // two projections into one y would race
-    a.h_out[i] = h_outs[i];
     a.w[i] = ws[i];
     a.w_scales[i] = w_scales[i];
     a.y[i] = ys[i];
   }
-  return launch_dense(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
+  DensePlan plan;
+  if (!plan_dense(a, compute_units(), &plan)) return SGMV_ERR_UNSUPPORTED;
+  return launch_dense(a, plan, static_cast<hipStream_t>(stream)) == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
+}
+
+int sgmv_plan_dense_q8(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, const int32_t* h_outs,
+                       const void* workspace, size_t workspace_bytes, sgmv_plan* plan) {
+  if (plan == nullptr) return SGMV_ERR_NULL;
+  *plan = sgmv_plan{};
+  bool nothing = false;
+  const int rc = check_dense(dtype, n_proj, n_tokens, h_in, h_outs, workspace, &nothing);
+  if (rc != SGMV_OK || nothing) return rc;
+  DensePlan d;
+  if (!plan_dense(dense_shape(dtype, n_proj, n_tokens, h_in, h_outs, const_cast<void*>(workspace), workspace_bytes), compute_units(), &d))
+    return SGMV_ERR_UNSUPPORTED;
+  plan->kernel = d.family == kDenseFew ? SGMV_KERNEL_DENSE_FEW : d.family == kDenseSmall ? SGMV_KERNEL_DENSE_SMALL : SGMV_KERNEL_DENSE_LARGE;
+  plan->launches = d.splits > 1 ? 2 : 1;
+  plan->slices = d.splits;
+  plan->workgroups = (int32_t)d.workgroups;
+  plan->lds_bytes = d.lds;
+  return SGMV_OK;
 }
 
 }  // extern "C"

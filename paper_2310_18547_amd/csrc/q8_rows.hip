@@ -152,18 +152,28 @@ hipError_t launch_kind(const RowsArgs& a, hipStream_t st) {
   while (chunks < 4 && pieces > 1024 * chunks) chunks *= 2;
   while (chunks > 1 && pieces <= 64 * (chunks / 2)) chunks /= 2;
   const int threads = ((pieces + chunks - 1) / chunks + 63) / 64 * 64;
-  const dim3 grid((unsigned)a.n_tokens), block((unsigned)threads);
-  auto launch = [&](auto kernel) {
-    kernel<<<grid, block, 0, st>>>(static_cast<const uint16_t*>(a.x), static_cast<const uint16_t*>(a.other),
-                                   static_cast<const uint16_t*>(a.weight), static_cast<uint16_t*>(a.sum),
-                                   static_cast<uint16_t*>(a.out), a.q, a.q_scales, a.h, a.eps);
+  auto launch = [&](auto kernel) -> hipError_t {
+    auto at = [](auto* p, size_t offset) { return p == nullptr ? nullptr : p + offset; };
+    // a launch takes fewer than 2^32 threads
+    const int most = (1 << 30) / threads;
+    for (int first = 0; first < a.n_tokens;) {
+      const int rows = a.n_tokens - first < most ? a.n_tokens - first : most;
+      const size_t offset = (size_t)first * a.h;
+      kernel<<<(unsigned)rows, threads, 0, st>>>(at(static_cast<const uint16_t*>(a.x), offset), at(static_cast<const uint16_t*>(a.other), offset),
+                                                 static_cast<const uint16_t*>(a.weight), at(static_cast<uint16_t*>(a.sum), offset),
+                                                 at(static_cast<uint16_t*>(a.out), offset), at(a.q, offset), at(a.q_scales, (size_t)first),
+                                                 a.h, a.eps);
+      const hipError_t err = hipGetLastError();
+      if (err != hipSuccess) return err;
+      first += rows;
+    }
+    return hipSuccess;
   };
   switch (chunks) {
-    case 1: launch(rows_q8_kernel<DT, KIND, 1>); break;
-    case 2: launch(rows_q8_kernel<DT, KIND, 2>); break;
-    default: launch(rows_q8_kernel<DT, KIND, 4>); break;
+    case 1: return launch(rows_q8_kernel<DT, KIND, 1>);
+    case 2: return launch(rows_q8_kernel<DT, KIND, 2>);
+    default: return launch(rows_q8_kernel<DT, KIND, 4>);
   }
-  return hipGetLastError();
 }
 
 template <class DT>
