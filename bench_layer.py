@@ -16,6 +16,10 @@ library's kernels, issued three ways:
 * ``lora_single``     + seven ``sgmv_add_lora`` calls;
 * ``lora_multi``      + ``sgmv_add_lora_multi`` for q/k/v and for gate/up, single calls for o, down.
 
+``--backbone q8`` holds the layer's own weights in 8-bit integers instead (``layer.Q8Layer``): the projections are
+this library's kernels too, and a step is the whole layer but attention -- norms, 8-bit rows, gated activation and
+the seven projections -- without (``backbone``) and with the add-ons (``lora_multi``).
+
 Consecutive steps cycle over ``--layers`` sets of backbone and adapter weights so that nothing
 is served from the on-die caches.  Everything is synthetic (random weights, as in the paper's
 microbenchmarks).  Prints ONE JSON line.  This follows the paper's transformer-layer
@@ -43,6 +47,7 @@ def main():
     ap.add_argument("--mix", choices=["distinct", "uniform", "skewed", "identical"], default="distinct",
                     help="adapter popularity over the --batch decode rows (the operator microbenchmark's mixes): "
                          "rows that share an adapter form one segment")
+    ap.add_argument("--backbone", choices=["f16", "q8"], default="f16", help="the layer's own weights: 16-bit floats or 8-bit integers")
     ap.add_argument("--rank", type=int, default=16)
     ap.add_argument("--layers", type=int, default=4, help="weight sets cycled through")
     ap.add_argument("--steps", type=int, default=200)
@@ -171,19 +176,36 @@ def main():
                 ts.append(e0.elapsed_time(e1) / K * 1e3)
         return float(np.median(ts))
 
-    res = {"backbone_us": timeit(step_backbone), "lora_single_us": timeit(step_single),
-           "lora_multi_us": timeit(step_multi), "lora_only_multi_us": timeit(lora_only_multi)}
-    assert B.sgmv_workspace_check(ws, sh) == 0
-    weights = sum(i * o for i, o in shapes.values()) * 2
+    if args.backbone == "q8":
+        from paper_2310_18547_amd.layer import Q8Layer, quantize_weight
+        w8 = {n: [tuple(t.contiguous() for t in quantize_weight(w.t())) for w in W[n]] for n in shapes}
+        norms = [tuple(torch.ones(h, dtype=f16, device=dev) for _ in range(2)) for _ in range(L)]
+        layer = Q8Layer(h, ffn, r, L, T, B.F16, A_ptrs, B_ptrs, seg_starts, n_req, max(seg_lens), w8, norms, device=dev)
+        residual, attention = rnd(T, h), rnd(T, h)
+
+        def step_q8(i):
+            layer.qkv(None, residual, i % L, stream=sh)
+            layer.finish(attention, residual, i % L, stream=sh)
+
+        layer.add_ons = False
+        res = {"backbone_us": timeit(step_q8)}
+        layer.add_ons = True
+        res["lora_multi_us"] = timeit(step_q8)
+        assert layer.check(sh) == 0
+    else:
+        res = {"backbone_us": timeit(step_backbone), "lora_single_us": timeit(step_single),
+               "lora_multi_us": timeit(step_multi), "lora_only_multi_us": timeit(lora_only_multi)}
+        assert B.sgmv_workspace_check(ws, sh) == 0
+    weights = sum(i * o for i, o in shapes.values()) * (1 if args.backbone == "q8" else 2)
     lora = sum((i * r + r * o) for i, o in shapes.values()) * 2 * n_req
-    out = {"benchmark": "decoder-layer dense projections + LoRA add-ons",
+    out = {"benchmark": "decoder-layer dense projections + LoRA add-ons", "backbone": args.backbone,
            "model": args.model, "h": h, "ffn": ffn, "batch": args.batch, "seq": args.seq, "mix": args.mix,
            "adapters": n_req, "tokens": T, "rank": r,
            "layers_cycled": L,
            "steps": args.steps, "dtype": "f16", "data": "synthetic", "n_gpus": 1,
            "backbone_weight_bytes_per_step": weights, "adapter_weight_bytes_per_step": lora,
            **res,
-           "lora_overhead_single_us": res["lora_single_us"] - res["backbone_us"],
+           **({"lora_overhead_single_us": res["lora_single_us"] - res["backbone_us"]} if "lora_single_us" in res else {}),
            "lora_overhead_multi_us": res["lora_multi_us"] - res["backbone_us"],
            "lora_overhead_multi_frac": res["lora_multi_us"] / res["backbone_us"] - 1.0}
     print(json.dumps(out), flush=True)

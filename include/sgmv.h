@@ -418,7 +418,8 @@ int sgmv_quantize_q8(int32_t dtype, int8_t* q, float* q_scales, const void* x, i
  *   ws        HOST array of device pointers, w_i int8 [h_outs[i]][h_in] (an output channel's weights
  *             in a row)
  *   w_scales  HOST array of device pointers, fp32 [h_outs[i]]
- *   h_outs    HOST array of output widths, at most 2^27 (n_tokens at most 2^30; else SGMV_ERR_UNSUPPORTED)
+ *   h_outs    HOST array of output widths, at most 2^27 (n_tokens at most 2^30, and 2^38
+ *             values of y in all; else SGMV_ERR_UNSUPPORTED)
  *   workspace device scratch, 256-byte aligned, or NULL with 0 bytes.  Shapes with few output tiles
  *             and a long h_in divide the sum over more workgroups where their partial sums (4 bytes for
  *             every value of y and part) fit in it; SGMV_DENSE_WORKSPACE_BYTES is enough for nearly all

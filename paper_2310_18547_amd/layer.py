@@ -7,6 +7,10 @@ segment indices in the section on the runner).  ``LoraLayer`` issues those seven
 through the C ABI: the projections that read the same activations (q/k/v, gate/up) go into
 one ``sgmv_add_lora_multi`` call each, o and down are single ``sgmv_add_lora`` calls.  All
 calls share one workspace and must be enqueued on one stream.
+
+``Q8Layer`` is a layer whose own weights are held in 8-bit integers: besides the add-ons it
+issues the norms, the dense projections and the gated activation that they stand between,
+everything of the layer but attention.
 """
 from __future__ import annotations
 
@@ -58,3 +62,77 @@ class LoraLayer:
 
     def check(self, stream=None) -> int:
         return B.sgmv_workspace_check(self.workspace, stream)
+
+
+def quantize_weight(w: torch.Tensor):
+    """A projection's weight ``[h_out, h_in]`` in 8-bit integers with a scale per output channel (once, at loading)."""
+    top = w.float().abs().amax(1, keepdim=True)
+    scales = torch.where(top > 0, top / 127.0, torch.ones_like(top))
+    return torch.round(w.float() / scales).to(torch.int8).contiguous(), scales[:, 0].contiguous()
+
+
+class Q8Layer(LoraLayer):
+    """A decoder layer with an 8-bit backbone and 16-bit LoRA add-ons, for batches of ``n_tokens`` rows.
+
+    ``weights`` holds, for every name of ``PROJECTIONS``, a list with a layer's ``(int8 [h_out, h_in], fp32 [h_out])`` for every
+    layer; ``norms`` the 16-bit norm weights of every layer, ``(in front of attention, in front of the MLP)``.  The
+    buffers are the object's own and are used again by the next call: one call at a time, on one stream.
+    """
+
+    def __init__(self, h: int, ffn: int, r: int, num_layers: int, n_tokens: int, dtype: int, A_ptrs, B_ptrs, seg_starts,
+                 n_segs: int, max_seg_len: int, weights, norms, eps: float = 1e-5, device="cuda:0"):
+        super().__init__(h, ffn, r, num_layers, n_tokens, dtype, A_ptrs, B_ptrs, seg_starts, n_segs, max_seg_len, device)
+        self.dtype, self.n_tokens, self.h, self.ffn, self.eps = dtype, n_tokens, h, ffn, eps
+        self.weights, self.norms = weights, norms
+        self.add_ons = True  # False: the backbone alone (benchmarks compare the two)
+        for name, (h_in, h_out) in self.shapes.items():
+            for w, s in weights[name]:
+                assert w.dtype == torch.int8 and w.shape == (h_out, h_in) and w.is_contiguous(), name
+                assert s.dtype == torch.float32 and s.shape == (h_out,) and s.is_contiguous(), name
+        kind = torch.float16 if dtype == B.F16 else torch.bfloat16
+
+        def rows(width, kind=kind):
+            return torch.empty(n_tokens, width, dtype=kind, device=device)
+
+        self.y = {name: rows(h_out) for name, (_, h_out) in self.shapes.items()}
+        self.x, self.act = rows(h), rows(ffn)                            # normed rows, gated activations
+        self.q, self.q_ffn = rows(h, torch.int8), rows(ffn, torch.int8)  # in 8 bits
+        self.q_scales = torch.empty(n_tokens, dtype=torch.float32, device=device)
+        self.scratch = torch.empty(B.DENSE_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+    def dense(self, names: Sequence[str], q, layer_idx: int, stream=None) -> None:
+        """Projections of the same 8-bit rows into ``self.y``, without their add-ons."""
+        pairs = [self.weights[n][layer_idx] for n in names]
+        B.sgmv_dense_q8(self.dtype, [self.y[n] for n in names], q, self.q_scales, [w for w, _ in pairs], [s for _, s in pairs],
+                        self.n_tokens, self.shapes[names[0]][0], [self.shapes[n][1] for n in names], self.scratch,
+                        self.scratch.numel(), stream)
+
+    def project(self, names: Sequence[str], q, x, layer_idx: int, scale: float = 1.0, stream=None) -> None:
+        """Projections of the same rows, ``q`` in 8 bits and ``x`` in 16, and their add-ons, into ``self.y``."""
+        self.dense(names, q, layer_idx, stream)
+        if self.add_ons:
+            self.add_lora_group(names, [self.y[n] for n in names], [x] * len(names), layer_idx, scale, stream)
+
+    def norm(self, which: int, x, residual, layer_idx: int, stream=None) -> None:
+        """``residual += x`` (in place), its norm into ``self.x`` and ``self.q``; ``which``: 0 attention's, 1 the MLP's.  ``x`` None:
+        the residual as it is."""
+        s = residual if x is None else x
+        B.sgmv_rms_norm_q8(self.dtype, self.x, self.q, self.q_scales, None if x is None else residual, s,
+                           None if x is None else residual, self.norms[layer_idx][which], self.eps, self.n_tokens, self.h, stream)
+
+    def qkv(self, x, residual, layer_idx: int, scale: float = 1.0, stream=None):
+        """Up to attention: norm, q / k / v with their add-ons."""
+        self.norm(0, x, residual, layer_idx, stream)
+        self.project(("q", "k", "v"), self.q, self.x, layer_idx, scale, stream)
+        return self.y["q"], self.y["k"], self.y["v"]
+
+    def finish(self, attention, residual, layer_idx: int, scale: float = 1.0, stream=None):
+        """From attention's output on: o, norm, gate / up, activation, down.  Returns what the next layer adds to the residual."""
+        B.sgmv_quantize_q8(self.dtype, self.q, self.q_scales, attention, self.n_tokens, self.h, stream)
+        self.project(("o",), self.q, attention, layer_idx, scale, stream)
+        self.norm(1, self.y["o"], residual, layer_idx, stream)
+        self.project(("gate", "up"), self.q, self.x, layer_idx, scale, stream)
+        B.sgmv_silu_mul_q8(self.dtype, self.act, self.q_ffn, self.q_scales, self.y["gate"], self.y["up"], self.n_tokens, self.ffn,
+                           stream)
+        self.project(("down",), self.q_ffn, self.act, layer_idx, scale, stream)
+        return self.y["down"]

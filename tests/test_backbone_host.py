@@ -91,3 +91,50 @@ def test_calls_take_keywords_and_every_form_of_argument():
     assert sg.sgmv_dense_q8(sg.F16, (), FAKE, FAKE, [], (), 4, 64, []) == 0
     assert sg.sgmv_dense_q8(sg.F16, [FAKE, FAKE * 2], FAKE, FAKE, [FAKE], [FAKE, FAKE], 4, 64, [8, 8], check=False) == NULL
     assert sg.DENSE_WORKSPACE_BYTES == 16 << 20
+
+
+def _plan(n, h_in, h_outs, nbytes=0, **kw):
+    return sg.sgmv_plan_dense_q8(sg.F16, n, h_in, h_outs, FAKE if nbytes else None, nbytes, **kw)
+
+
+def test_plan_dense():
+    """Which kernel serves a call: few tokens, small and large tiles, the sum divided where a workspace holds the parts."""
+    p = _plan(1, 4096, [4096] * 3)
+    assert p.kernel == sg.KERNEL_DENSE_FEW and p.launches == 1 and p.slices == 1 and 0 < p.lds_bytes <= 160 * 1024
+    assert _plan(64, 4096, [4096]).kernel == sg.KERNEL_DENSE_FEW
+    p = _plan(517, 4096, [4096, 1024, 1024])
+    assert p.kernel == sg.KERNEL_DENSE_SMALL and p.workgroups == 5 * (32 + 8 + 8)
+    p = _plan(4814, 8192, [28672], 16 << 20)
+    assert p.kernel == sg.KERNEL_DENSE_LARGE and p.launches == 1 and p.workgroups == 19 * 112
+    alone, joined = _plan(256, 13824, [5120]), _plan(256, 13824, [5120], 16 << 20)
+    assert alone.launches == 1 and alone.slices == 1 and joined.launches == 2 and joined.slices > 1
+    parts = joined.slices * 256 * 5120 * 4
+    assert _plan(256, 13824, [5120], parts).slices == joined.slices and _plan(256, 13824, [5120], parts - 1).slices < joined.slices
+    p = _plan(0, 64, [64])
+    assert p.kernel == 0 and p.launches == 0
+    for bad, rc in ((dict(n=1, h_in=12, h_outs=[8]), UNSUPPORTED), (dict(n=-1, h_in=8, h_outs=[8]), SHAPE),
+                    (dict(n=1, h_in=8, h_outs=[12]), UNSUPPORTED), (dict(n=1, h_in=8, h_outs=[8] * 9), SHAPE),
+                    (dict(n=(1 << 30) + 8, h_in=8, h_outs=[8]), UNSUPPORTED), (dict(n=1, h_in=8, h_outs=[(1 << 27) + 8]), UNSUPPORTED)):
+        assert _plan(**bad, check=False)[0] == rc
+    assert sg.lib.sgmv_plan_dense_q8(0, 1, 1, 8, None, None, 0, None) == NULL
+    with pytest.raises(sg.SgmvError, match="sgmv_plan_dense_q8"):
+        _plan(1, 12, [8])
+
+
+def test_every_dense_kernel_is_reached_and_fits():
+    """Over usual sizes every kernel of the table is the choice for some; grids and LDS stay within what a launch takes."""
+    seen = {}
+    for n in (1, 3, 16, 17, 32, 33, 45, 48, 64, 65, 96, 128, 200, 256, 384, 517, 768, 1024, 2048, 4814, 1 << 22, 1 << 30):
+        for h_in in (8, 1024, 4096, 4104, 13824, 131064):
+            for h_outs in ([8], [1024], [2048], [4096], [4096] * 3, [11008] * 2, [5120], [28672], [1 << 27]):
+                for nbytes in (0, 16 << 20):
+                    rc, p = _plan(n, h_in, h_outs, nbytes, check=False)
+                    if rc != 0:
+                        assert rc == UNSUPPORTED and n * sum(h_outs) > 1 << 38, (n, h_in, h_outs)
+                        continue
+                    assert p.lds_bytes <= 160 * 1024 and 1 <= p.slices <= 8 and (p.slices == 1 or nbytes)
+                    seen.setdefault((p.kernel, p.lds_bytes), (n, h_in, h_outs))
+    # few tokens: rings of 80 K to 160 K; small tiles 64 x 32, 64 x 64, 64 x 128, 128 x 128; large 64 K, 96 K and 128 K
+    assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_SMALL} == {72, 96, 120, 160}, seen
+    assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_LARGE} == {64, 96, 128}, seen
+    assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_FEW} == {80, 96, 128, 160}, seen

@@ -206,6 +206,66 @@ def test_dense_every_tail(h_in, dtype):
                 assert same, (n, h_in, w.shape)
 
 
+# (tokens, h_in, h_outs, workspace, kernel, LDS, parts of the sum): every kernel of the dense call, an even and an odd number of
+# whole steps, with and without a shorter one behind them
+EVERY_KERNEL = [
+    (1, 1136, (8,), 1, 9, 131072, 1),
+    (1, 1152, (8,), 1, 9, 131072, 1),
+    (266, 1400, (10552, 5976), 0, 11, 65536, 1),
+    (269, 1152, (9600, 7904), 0, 11, 65536, 1),
+    (40, 9296, (24, 8408), 1, 11, 65536, 7),
+    (36, 10728, (7032, 2848), 1, 11, 65536, 6),
+    (67, 1280, (9832, 7320), 0, 10, 163840, 1),
+    (67, 1152, (10160, 6576), 1, 10, 163840, 1),
+    (2735, 5976, (216,), 1, 10, 163840, 5),
+    (75, 5096, (280, 5504), 1, 10, 163840, 4),
+    (133, 1280, (9080, 9104), 1, 11, 98304, 1),
+    (131, 1160, (4424, 13208), 1, 11, 98304, 1),
+    (138, 4424, (8816,), 1, 11, 98304, 3),
+    (2704, 10984, (80, 8), 1, 11, 98304, 8),
+    (114, 1136, (544,), 0, 9, 98304, 1),
+    (81, 1152, (680,), 0, 9, 98304, 1),
+    (76, 1144, (1544, 88), 1, 9, 131072, 1),
+    (97, 1152, (1160,), 0, 9, 131072, 1),
+    (35, 1280, (6184,), 1, 9, 81920, 1),
+    (34, 1152, (296, 5816), 1, 9, 81920, 1),
+    (516, 1280, (13688, 8), 1, 11, 131072, 1),
+    (269, 1160, (9344, 13288), 1, 11, 131072, 1),
+    (98, 1280, (16, 2312), 0, 9, 81920, 1),
+    (116, 1160, (2000, 48), 1, 9, 81920, 1),
+    (1, 1136, (8848,), 1, 9, 81920, 1),
+    (1, 1152, (7208, 1024), 1, 9, 81920, 1),
+    (33, 1280, (3568, 13200), 0, 9, 163840, 1),
+    (68, 1160, (8320, 8), 1, 9, 163840, 1),
+    (2865, 1400, (264, 8), 0, 10, 122880, 1),
+    (2897, 1152, (8, 280), 0, 10, 122880, 1),
+    (2718, 11848, (8,), 1, 10, 122880, 8),
+    (2974, 9208, (8,), 1, 10, 122880, 8),
+    (131, 1280, (8,), 0, 10, 73728, 1),
+    (129, 1152, (8,), 1, 10, 73728, 1),
+    (1, 6720, (8,), 1, 10, 73728, 6),
+    (6, 6880, (8,), 1, 10, 73728, 6),
+    (2862, 1400, (8, 80), 1, 10, 98304, 1),
+    (2730, 1152, (72, 8), 1, 10, 98304, 1),
+    (2075, 4152, (8,), 1, 10, 98304, 4),
+    (2832, 4008, (8,), 1, 10, 98304, 3),
+]
+
+
+@pytest.mark.parametrize("n,h_in,h_outs,scratch,kernel,lds,parts", EVERY_KERNEL)
+def test_dense_every_kernel(n, h_in, h_outs, scratch, kernel, lds, parts):
+    from paper_2310_18547_amd import binding as B
+    workspace = torch.full((16 << 20,), 0x5A, dtype=torch.uint8, device="cuda:0") if scratch else None
+    plan = B.sgmv_plan_dense_q8(B.F16, n, h_in, h_outs, workspace, 16 << 20 if scratch else 0)
+    assert (plan.kernel, plan.lds_bytes, plan.slices) == (kernel, lds, parts)
+    rng = np.random.default_rng(n + h_in)
+    for dtype in ("f16", "bf16"):
+        inputs = _dense_inputs(rng, n, h_in, h_outs)
+        for y, w, s in zip(_dense(dtype, *inputs, workspace=workspace), inputs[2], inputs[3]):
+            same = np.array_equal(y, ref.dense(inputs[0], inputs[1], w, s, dtype))
+            assert same, (dtype, w.shape)
+
+
 @pytest.mark.parametrize("n,h_in,h_outs", [(1, 4096, (4096, 4096, 4096)), (7, 13824, (5120,)), (64, 4096, (2752, 2752)),
                                            (65, 11008, (1024,)), (130, 4104, (520, 1032)), (517, 2048, (1024, 256, 256)),
                                            (1031, 1024, (1288,)), (2100, 520, (2048,)), (2100, 512, (2056,)), (64, 131064, (24,)),
@@ -276,6 +336,30 @@ def test_offsets_past_32_bits():
     rows = [0, n // 2, n - 1]
     v = x[rows].double().cpu().numpy()
     ref.check_rows(v, None, _host(q[rows]), _host(scales[rows]).astype(np.float64), "bf16")
+
+
+def test_two_streams_at_once():
+    """Dense calls on two streams, with workspaces of their own, do not disturb each other."""
+    from paper_2310_18547_amd import binding as B
+    rng = np.random.default_rng(21)
+    n, h_in, h_out = 100, 8192, 1032
+    assert B.sgmv_plan_dense_q8(B.F16, n, h_in, [h_out], 0x10000, 16 << 20).slices > 1
+    jobs = []
+    for _ in range(2):
+        q, qs, ws, ss = _dense_inputs(rng, n, h_in, (h_out,))
+        jobs.append(dict(want=ref.dense(q, qs, ws[0], ss[0], "f16"), q=_dev(q), qs=_dev(qs), w=_dev(ws[0]), s=_dev(ss[0]),
+                         y=[_marked(n, h_out) for _ in range(20)], stream=torch.cuda.Stream(device="cuda:0"),
+                         scratch=torch.empty(16 << 20, dtype=torch.uint8, device="cuda:0")))
+    torch.cuda.synchronize()
+    for i in range(20):
+        for j in jobs:
+            B.sgmv_dense_q8(B.F16, [j["y"][i]], j["q"], j["qs"], [j["w"]], [j["s"]], n, h_in, [h_out], j["scratch"], 16 << 20, j["stream"])
+    torch.cuda.synchronize()
+    for j in jobs:
+        for y in j["y"]:
+            _behind(y, n)
+            same = np.array_equal(_host(y)[:n], j["want"])
+            assert same
 
 
 def test_streams_graphs_and_repeated_calls():
