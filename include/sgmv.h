@@ -377,7 +377,7 @@ int sgmv_plan_expand(const sgmv_problem* p, int32_t n_segs, sgmv_plan* plan);
  *
  * Conventions beyond the general ones above:
  *   - 8-bit rows are int8 [n_tokens][h] with fp32 scales [n_tokens]: they stand for q * scale.
- *     For row values v, top = max |v|: scale = top / 127 and q = v * (127 / top) rounded to the
+ *     For row values v, top = max |v|: scale = top / 127 and q = v * (1 / top * 127) rounded to the
  *     nearest, ties to even, so |q| <= 127.  A row of zeros has scale 0 and zeros.  A row in which
  *     a value is not finite has scale NaN and zeros, so every product with it is NaN.
  *   - Between the 16-bit loads and the stores everything is fp32, each output rounded once.

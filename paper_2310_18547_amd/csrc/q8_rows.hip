@@ -4,7 +4,7 @@
 //   norm      s = x + residual;  v = s * rsqrt(mean(s^2) + eps) * weight
 //   silu      v = gate / (1 + exp(-gate)) * up
 //   quantize  v = x
-//   8 bits    top = max |v|;  scale = top / 127;  q = v * (127 / top), rounded to the nearest even
+//   8 bits    top = max |v|;  scale = top / 127;  q = v * (1 / top * 127), rounded to the nearest even
 //
 // All of it is fp32 between the 16-bit loads and the stores.  In the norm the factor rsqrt(...) is common to the
 // row and cancels in q, so the row's maximum is taken of |s * weight| and one reduction of two numbers serves both:
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* __restric
     q_scales[blockIdx.x] = finite ? inv * peak / 127.0f : __uint_as_float(0x7FC00000u);
   // 127 / peak leaves fp32's range for the smallest peaks: those rows are made larger first
   const float up = peak < 0x1p-60f ? 0x1p64f : 1.0f;
-  const float factor = finite && top != 0 ? 127.0f / (peak * up) : 0.0f;
+  const float factor = finite && top != 0 ? 1.0f / (peak * up) * 127.0f : 0.0f;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int at = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
@@ -146,11 +146,11 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* __restric
 
 template <class DT, RowsKind KIND>
 hipError_t launch_kind(const RowsArgs& a, hipStream_t st) {
-  // threads of a row: few rows want a row's loads spread over as many lanes as it has pieces, many rows fewer, fuller waves
+  // Pieces of a row to a thread: one up to 512 threads to a row, then two, four where these are not enough.  Norms, one /
+  // two / four pieces, us: 4096 wide, 64 rows 3.6 / 4.1 / 4.8, 512 rows 6.3 / 6.7 / 7.6, 8192 rows 58.7 / 57.6 / 60.5; 8192 wide,
+  // 64 rows 4.6 / 4.5 / 5.2, 768 rows 15.6 / 13.8 / 14.0, 2048 rows 34.9 / 32.2 / 34.1.
   const int pieces = a.h / 8;
-  int chunks = a.n_tokens >= 512 ? 4 : 1;
-  while (chunks < 4 && pieces > 1024 * chunks) chunks *= 2;
-  while (chunks > 1 && pieces <= 64 * (chunks / 2)) chunks /= 2;
+  const int chunks = pieces <= 512 ? 1 : pieces <= 2048 ? 2 : 4;
   const int threads = ((pieces + chunks - 1) / chunks + 63) / 64 * 64;
   auto launch = [&](auto kernel) -> hipError_t {
     auto at = [](auto* p, size_t offset) { return p == nullptr ? nullptr : p + offset; };
