@@ -60,15 +60,25 @@ __device__ __forceinline__ uint2 finish4(i32x4 sum, float q_scale, const float* 
   return make_uint2(pack2<DT>(r[0], r[1]), pack2<DT>(r[2], r[3]));
 }
 
-// Sixteen bytes of every lane from `from` + its own offset + a common one into consecutive places of LDS.  In assembly
-// because the compiler, which cannot tell the two buffers apart, waits for every such load in front of every LDS read;
-// arrive() does the waiting.  The instruction writes no register but m0, which nothing else here uses.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t lane_off, uint32_t uniform_off, const int8_t* to) {
+// N loads, each of sixteen bytes of every lane from `from` + the lane's own offset + a common one into 1024 consecutive bytes of
+// LDS, the first to `to` and each STRIDE bytes behind the one before.  In assembly because the compiler, which cannot tell the
+// places of the ring apart, waits for every such load in front of every LDS read; arrive() does the waiting.  The loads write no
+// register but m0, which nothing else here uses.  The five wait states (s_nop 4) are those that a load needs behind a vector
+// instruction that has written one of its scalar operands, which the compiler does not see to in front of assembly.
+template <int N, int STRIDE>
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, const uint32_t (&lane_off)[N], uint32_t uniform_off, const int8_t* to) {
   const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) int8_t*)to);
   uniform_off = (uint32_t)__builtin_amdgcn_readfirstlane((int)uniform_off);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(lane_off), "s"(from),
-               "s"(uniform_off)
-               : "memory");
+#pragma unroll
+  for (int i = 0; i + 1 < N; i += 2)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds\n\t"
+                 "s_add_u32 m0, m0, %5\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %2, %3 offen lds" ::"s"(at + i * STRIDE), "v"(lane_off[i]), "s"(from),
+                 "s"(uniform_off), "v"(lane_off[i + 1]), "n"(STRIDE)
+                 : "memory", "scc");
+  if constexpr (N % 2 != 0)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at + (N - 1) * STRIDE), "v"(lane_off[N - 1]),
+                 "s"(from), "s"(uniform_off)
+                 : "memory");
 }
 // Waits until all but this many of the wave's loads have arrived and its LDS reads are done, then for the other waves.
 template <int LEFT>
@@ -159,11 +169,8 @@ struct DenseWork {
   }
   // All of a step into the ring.
   __device__ __forceinline__ void fetch(int step, int place) const {
-#pragma unroll
-    for (int i = 0; i < T::kLoadsW; ++i) load_to_lds(from_w, off_w[i], (uint32_t)step * 128u, lds + place + (i * T::kWaves + wave) * 1024);
-#pragma unroll
-    for (int i = 0; i < T::kLoadsQ; ++i)
-      load_to_lds(from_q, off_q[i], (uint32_t)step * 128u, lds + place + T::kChannels * 128 + (i * T::kWaves + wave) * 1024);
+    load_to_lds<T::kLoadsW, T::kWaves * 1024>(from_w, off_w, (uint32_t)step * 128u, lds + place + wave * 1024);
+    load_to_lds<T::kLoadsQ, T::kWaves * 1024>(from_q, off_q, (uint32_t)step * 128u, lds + place + T::kChannels * 128 + wave * 1024);
   }
   // The shorter step at the end into the first place, through registers: zeros behind the rows' ends.
   __device__ __forceinline__ void fetch_rest() const {
@@ -234,6 +241,7 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void dense_q8_large_kernel(DenseTa
   using T = DenseTile<NC, NT, WC, WT, 2>;
   constexpr int kLoadsW = T::kLoadsW / 2, kLoadsQ = T::kLoadsQ / 2;  // of a half
   static_assert(T::kLoadsW % 2 == 0 && T::kLoadsQ % 2 == 0 && NC % 4 == 0 && NT % 2 == 0, "whole loads of half the rows");
+  static_assert(T::kWaves * 8 % (2 * NC) == 0 && T::kWaves * 8 % (8 * NT) == 0, "loads of a half lie evenly");
   extern __shared__ __align__(1024) int8_t lds[];
   const DenseWork<T, NC, NT, WC> work(t, q, shape, lds);
   // row j of a half: the first or second NC / 2 fragments of every wave's channels, NT / 2 of its tokens
@@ -254,16 +262,13 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void dense_q8_large_kernel(DenseTa
     }
   }
   auto fetch_w = [&](int step, int half) {
-    int8_t* to = lds + (step & 1) * T::kPlace;
-#pragma unroll
-    for (int i = 0; i < kLoadsW; ++i)
-      load_to_lds(work.from_w, off_w[half][i], (uint32_t)step * 128u, to + w_half_row(half, (i * T::kWaves + work.wave) * 8) * 128);
+    // a load further on is kWaves * 8 rows of the half, twice as many of the tile
+    load_to_lds<kLoadsW, T::kWaves * 2048>(work.from_w, off_w[half], (uint32_t)step * 128u,
+                                           lds + (step & 1) * T::kPlace + w_half_row(half, work.wave * 8) * 128);
   };
   auto fetch_q = [&](int step, int half) {
-    int8_t* to = lds + (step & 1) * T::kPlace + T::kChannels * 128;
-#pragma unroll
-    for (int i = 0; i < kLoadsQ; ++i)
-      load_to_lds(work.from_q, off_q[half][i], (uint32_t)step * 128u, to + q_half_row(half, (i * T::kWaves + work.wave) * 8) * 128);
+    load_to_lds<kLoadsQ, T::kWaves * 2048>(work.from_q, off_q[half], (uint32_t)step * 128u,
+                                           lds + (step & 1) * T::kPlace + (T::kChannels + q_half_row(half, work.wave * 8)) * 128);
   };
   i32x4 acc[NC][NT] = {};
   uint4 fw[2][NC / 2], fq[2][2][NT / 2];
@@ -453,10 +458,8 @@ __global__ __launch_bounds__(64 * WAVES) void dense_q8_few_kernel(DenseTable t, 
   int8_t* ring = lds + wave * (DEPTH * T::kPlace);
   auto fetch = [&](int chunk, int place) {
     int8_t* to = ring + place * T::kPlace;
-#pragma unroll
-    for (int i = 0; i < 2 * CH; ++i) load_to_lds(from_w, off_w[i], chunk * 128, to + i * 1024);
-#pragma unroll
-    for (int i = 0; i < 2 * NT; ++i) load_to_lds(from_q, off_q[i], chunk * 128, to + (2 * CH + i) * 1024);
+    load_to_lds<2 * CH, 1024>(from_w, off_w, (uint32_t)chunk * 128u, to);
+    load_to_lds<2 * NT, 1024>(from_q, off_q, (uint32_t)chunk * 128u, to + CH * 2048);
   };
   i32x4 acc[CH][NT] = {};
   const int piece = ((lane >> 4) ^ (lane >> 1 & 7)) * 16;

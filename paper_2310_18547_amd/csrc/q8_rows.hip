@@ -148,9 +148,10 @@ template <class DT, RowsKind KIND>
 hipError_t launch_kind(const RowsArgs& a, hipStream_t st) {
   // Pieces of a row to a thread: one up to 512 threads to a row, then two, four where these are not enough.  Norms, one /
   // two / four pieces, us: 4096 wide, 64 rows 3.6 / 4.1 / 4.8, 512 rows 6.3 / 6.7 / 7.6, 8192 rows 58.7 / 57.6 / 60.5; 8192 wide,
-  // 64 rows 4.6 / 4.5 / 5.2, 768 rows 15.6 / 13.8 / 14.0, 2048 rows 34.9 / 32.2 / 34.1.
+  // 64 rows 4.6 / 4.5 / 5.2, 768 rows 15.6 / 13.8 / 14.0, 2048 rows 34.9 / 32.2 / 34.1.  Plain rows, with one load to a piece,
+  // take two in larger batches too: 4096 wide, 1024 rows 4.7 / 4.9 / 5.0, 2048 rows 7.5 / 6.9 / 7.1, 8192 rows 19.7 / 17.4 / 17.2.
   const int pieces = a.h / 8;
-  const int chunks = pieces <= 512 ? 1 : pieces <= 2048 ? 2 : 4;
+  const int chunks = pieces > 2048 ? 4 : pieces > 512 || (KIND == kRowsQuantize && pieces > 64 && a.n_tokens >= 2048) ? 2 : 1;
   const int threads = ((pieces + chunks - 1) / chunks + 63) / 64 * 64;
   auto launch = [&](auto kernel) -> hipError_t {
     auto at = [](auto* p, size_t offset) { return p == nullptr ? nullptr : p + offset; };
