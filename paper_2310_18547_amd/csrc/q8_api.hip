@@ -72,7 +72,7 @@ int sgmv_rms_norm_q8(int32_t dtype, void* out, int8_t* q, float* q_scales, void*
   rc = check_q8(q, q_scales, false);
   if (rc != SGMV_OK) return rc;
   if (!aligned(out, 16) || !aligned(sum, 16) || !aligned(x, 16) || !aligned(residual, 16) || !aligned(weight, 16)) return SGMV_ERR_ALIGN;
-  if (out != nullptr && (out == sum || out == weight)) return SGMV_ERR_SHAPE;
+  if ((out != nullptr && (out == sum || out == weight)) || sum == weight) return SGMV_ERR_SHAPE;  // one would be lost
   return launch(RowsArgs{kRowsNorm, dtype == SGMV_BF16, n_tokens, h, eps, x, residual, weight, sum, out, q, q_scales}, stream);
 }
 

@@ -1,6 +1,7 @@
 """The 8-bit backbone calls without a GPU: what they refuse, and the forms of argument that they take."""
 import numpy as np
 import pytest
+import torch  # noqa: F401  (before the library, which the defaults below load: a process has one HIP runtime, torch's)
 
 import paper_2310_18547_amd as sg
 
@@ -44,6 +45,7 @@ def test_norm_refusals():
         assert _norm(**{name: 9 * FAKE + 8}) == ALIGN
     assert _norm(out=4 * FAKE) == SHAPE            # out is sum: one of the two would be lost
     assert _norm(out=5 * FAKE, sum=5 * FAKE) == SHAPE
+    assert _norm(sum=7 * FAKE) == SHAPE and _norm(out=7 * FAKE) == SHAPE   # over the weights that other rows read
 
 
 def test_silu_and_quantize_refusals():
