@@ -424,7 +424,8 @@ int sgmv_quantize_q8(int32_t dtype, int8_t* q, float* q_scales, const void* x, i
  *             and a long h_in divide the sum over more workgroups where their partial sums (4 bytes for
  *             every value of y and part) fit in it; SGMV_DENSE_WORKSPACE_BYTES is enough for nearly all
  *             that gain by it.  It needs no preparation, keeps nothing between calls, and calls that
- *             share it must be ordered.  The result is the same to the bit with any workspace. */
+ *             share it must be ordered; a prepared workspace of the add-ons is another buffer, which
+ *             this call would overwrite.  The result is the same to the bit with any workspace. */
 #define SGMV_DENSE_WORKSPACE_BYTES ((size_t)16 << 20)
 int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* q, const float* q_scales,
                   const int8_t* const* ws, const float* const* w_scales, int32_t n_tokens, int32_t h_in,

@@ -39,27 +39,33 @@ __device__ __forceinline__ V reduce_row(V v, V* of_waves, Join join) {
 
 // One workgroup per row, CHUNKS pieces of eight values to a thread.  grid = rows.
 template <class DT, RowsKind KIND, int CHUNKS>
-__global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* __restrict__ x, const uint16_t* other,
+__global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* x, const uint16_t* other,
                                                        const uint16_t* __restrict__ weight, uint16_t* sum_out, uint16_t* out,
                                                        int8_t* q, float* q_scales, int h, float eps) {
   __shared__ float sums[2][16];
   __shared__ uint32_t tops[16];
   const size_t base = (size_t)blockIdx.x * (size_t)h;
   float v[CHUNKS][8];
+  uint4 a[CHUNKS], b[CHUNKS];
   uint4 g[KIND == kRowsNorm ? CHUNKS : 1];  // the norm's weights, 16 bits each
+  // everything is loaded before anything is stored: outputs may lie where inputs do
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int at = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
-    uint4 a = make_uint4(0, 0, 0, 0), b = a;
-    if constexpr (KIND == kRowsNorm) g[c] = a;
+    a[c] = b[c] = make_uint4(0, 0, 0, 0);
+    if constexpr (KIND == kRowsNorm) g[c] = a[c];
     if (at < h) {
-      a = load128(x + base + at);
-      if (KIND == kRowsSiluMul || (KIND == kRowsNorm && other != nullptr)) b = load128(other + base + at);
+      a[c] = load128(x + base + at);
+      if (KIND == kRowsSiluMul || (KIND == kRowsNorm && other != nullptr)) b[c] = load128(other + base + at);
       if constexpr (KIND == kRowsNorm) g[c] = load128(weight + at);
     }
-    unpack8<DT>(a, v[c]);
+  }
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    const int at = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+    unpack8<DT>(a[c], v[c]);
     float t[8];
-    unpack8<DT>(b, t);
+    unpack8<DT>(b[c], t);
     if constexpr (KIND == kRowsNorm) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[c][i] += t[i];  // without a residual: + 0
@@ -143,12 +149,13 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* __restric
 
 template <class DT, RowsKind KIND>
 hipError_t launch_kind(const RowsArgs& a, hipStream_t st) {
-  // Pieces of a row to a thread: one up to 512 threads to a row, then two, four where these are not enough.  Norms, one /
-  // two / four pieces, us: 4096 wide, 64 rows 3.6 / 4.1 / 4.8, 512 rows 6.3 / 6.7 / 7.6, 8192 rows 58.7 / 57.6 / 60.5; 8192 wide,
-  // 64 rows 4.6 / 4.5 / 5.2, 768 rows 15.6 / 13.8 / 14.0, 2048 rows 34.9 / 32.2 / 34.1.  Plain rows, with one load to a piece,
-  // take two in larger batches too: 4096 wide, 1024 rows 4.7 / 4.9 / 5.0, 2048 rows 7.5 / 6.9 / 7.1, 8192 rows 19.7 / 17.4 / 17.2.
+  // Pieces of a row to a thread: two from 4096 wide on, or in large batches from 1024 wide on, one below; four where two are not
+  // enough.  One / two / four pieces, us: norm, 4096 wide, 64 rows 4.1 / 4.1 / 4.8, 512 rows 6.8 / 6.4 / 7.6, 8192 rows
+  // 58.4 / 57.2 / 58.9; 8192 wide, 768 rows 16.6 / 13.7 / 13.6, 2048 rows 33.7 / 31.4 / 32.4; 2048 wide, 512 rows 4.9 / 5.1 / 6.0,
+  // 8192 rows 30.6 / 30.4 / 31.0; plain rows, 4096 wide, 8192 rows 21.0 / 16.9 / 16.9, 1024 wide 7.3 / 6.4 / 6.8; 512 wide, 16384
+  // rows 7.0 / 7.2 / 8.1.
   const int pieces = a.h / 8;
-  const int chunks = pieces > 2048 ? 4 : pieces > 512 || (KIND == kRowsQuantize && pieces > 64 && a.n_tokens >= 2048) ? 2 : 1;
+  const int chunks = pieces > 2048 ? 4 : pieces >= 512 || (pieces >= 128 && a.n_tokens >= 2048) ? 2 : 1;
   const int threads = ((pieces + chunks - 1) / chunks + 63) / 64 * 64;
   auto launch = [&](auto kernel) -> hipError_t {
     auto at = [](auto* p, size_t offset) { return p == nullptr ? nullptr : p + offset; };

@@ -65,10 +65,14 @@ class LoraLayer:
 
 
 def quantize_weight(w: torch.Tensor):
-    """A projection's weight ``[h_out, h_in]`` in 8-bit integers with a scale per output channel (once, at loading)."""
-    top = w.float().abs().amax(1, keepdim=True)
-    scales = torch.where(top > 0, top / 127.0, torch.ones_like(top))
-    return torch.round(w.float() / scales).to(torch.int8).contiguous(), scales[:, 0].contiguous()
+    """A projection's weight ``[h_out, h_in]`` in 8-bit integers with a scale per output channel (once, at loading).
+    Weights that are not finite raise ``ValueError``."""
+    scales = w.float().abs().amax(1, keepdim=True) / 127.0
+    if not torch.isfinite(scales).all():
+        raise ValueError("weights that are not finite have no 8-bit form")
+    scales = torch.where(scales > 0, scales, torch.ones_like(scales))
+    # the smallest scales have few bits: a quotient may pass 127
+    return torch.round(w.float() / scales).clamp(-127, 127).to(torch.int8).contiguous(), scales[:, 0].contiguous()
 
 
 class Q8Layer(LoraLayer):

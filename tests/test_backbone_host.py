@@ -140,3 +140,16 @@ def test_every_dense_kernel_is_reached_and_fits():
     assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_SMALL} == {72, 96, 120, 160}, seen
     assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_LARGE} == {64, 96, 128}, seen
     assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_FEW} == {80, 96, 128, 160}, seen
+
+
+def test_quantize_weight():
+    from paper_2310_18547_amd.layer import quantize_weight
+    w = torch.tensor([[1.0, -2.0, 0.5, 0.0], [0.0] * 4, [1e-44, -1e-44, 3e-45, 0.0], [3e38, -1.0, 1.5e38, 0.0]])
+    q, s = quantize_weight(w)
+    assert q.dtype == torch.int8 and s.shape == (4,) and (s > 0).all()
+    assert q[0].tolist() == [64, -127, 32, 0] and not q[1].any() and not q[2].any() and q[3, 0] == 127  # 63.5: ties to even
+    for tiny in range(1, 400):  # multiples of fp32's smallest number
+        assert quantize_weight(torch.tensor([[tiny * 2.0 ** -149, -tiny * 2.0 ** -149]]))[0].sum() == 0
+    for bad in (float("inf"), float("nan")):
+        with pytest.raises(ValueError):
+            quantize_weight(torch.tensor([[1.0, bad]]))
