@@ -456,7 +456,13 @@ __global__ __launch_bounds__(64 * WAVES) void dense_q8_few_kernel(DenseTable t, 
     off_q[i] = (uint32_t)min(row, last_q) * (uint32_t)h_in + (uint32_t)(((lane & 7) ^ (row >> 1 & 7)) * 16);
   }
   int8_t* ring = lds + wave * (DEPTH * T::kPlace);
+  const int chunks = h_in / 128;
+  // The sum begins somewhere else in every workgroup: rows 4096 bytes apart would have all of them read from the same memory
+  // channels at once (4096 wide: one token, 3 x 4096 12.9 -> 11.8 us, 64 tokens, 2 x 11008 23.3 -> 22.3; 5120 and 8192 wide as without).
+  const int begin = chunks > 0 ? (int)(blockIdx.x * 11u % (unsigned)chunks) : 0;
   auto fetch = [&](int chunk, int place) {
+    chunk += begin;
+    if (chunk >= chunks) chunk -= chunks;
     int8_t* to = ring + place * T::kPlace;
     load_to_lds<2 * CH, 1024>(from_w, off_w, (uint32_t)chunk * 128u, to);
     load_to_lds<2 * NT, 1024>(from_q, off_q, (uint32_t)chunk * 128u, to + CH * 2048);
@@ -480,7 +486,6 @@ __global__ __launch_bounds__(64 * WAVES) void dense_q8_few_kernel(DenseTable t, 
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = mfma_i8(a[s][i], b[s][j], acc[i][j]);
   };
-  const int chunks = h_in / 128;
   constexpr int kLoads = 2 * (CH + NT);
   static_assert(kLoads * (DEPTH - 1) <= 63, "what the wait for loads can count");
   int fetched = wave;  // the chunk to fetch next
@@ -623,7 +628,7 @@ hipError_t launch_few(const DenseArgs& a, hipStream_t st) {
 // The kernels, and what the choice among them goes by: the time of a call is estimated for every one of them and the
 // shortest taken.  The figures below are fits to graph replays of 48 shapes (1 to 4814 tokens, h_in 1024 to 13824, outputs
 // of 1024 to 28672, weights from HBM), with every kernel each: the one chosen took 1.5 % more time than the best of them on
-// average, 10 % at worst (one token, 4096 -> 2 x 11008: 22.0 us against 20.0).
+// average, 10 % at worst.
 struct DenseKernel {
   int channels, tokens, threads, lds;
   // Few tokens, 0: a compute unit takes in 40 bytes of w and x a nanosecond, and the workgroups of a launch run in rounds of one to
