@@ -233,7 +233,8 @@ __device__ __forceinline__ void multiply(const uint4 (&fw)[NC], const uint4 (&fq
 // front of a product the half that it is the first to need is read from LDS, and a quarter of the step after next is fetched
 // into the place that the product before was the last to read: what is fetched has seven products' time to arrive.
 // PONG: eight waves in two groups, one of each to every SIMD, half a product apart: while one group multiplies, the other reads
-// and fetches.  Else several workgroups share a compute unit and fill each other's gaps.
+// and fetches (8192 tokens, 8192 -> 8192: 438 us, 2500 TOPS at 1.9 GHz, the matrix cores busy 64 % of the time: bound by power, as
+// a library's product is, 462 us at 1.6 GHz).  Else several workgroups share a compute unit and fill each other's gaps.
 // grid = tiles (channel tiles of all projections times token tiles)
 template <class DT, int NC, int NT, int WC, int WT, bool PONG>
 __global__ __launch_bounds__(64 * WC * WT, 2) void dense_q8_large_kernel(DenseTable t, const int8_t* __restrict__ q,
@@ -368,7 +369,8 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void dense_q8_large_kernel(DenseTa
   work.template store<DT>(t, q_scales, shape, acc);
 }
 
-// The kernel for smaller tiles.  While half a step's products run, the other half's or the next step's
+// The kernel for smaller tiles, bound by the compute units' intake (the fetches alone of 1024 tokens, 4096 -> 4096, take 19 of its
+// 25 us) and by some 100 to 190 clocks around a step's barrier.  While half a step's products run, the other half's or the next step's
 // fragments go from LDS to registers and a later step's pieces from memory to LDS; one barrier a step.
 // grid = tiles (channel tiles of all projections times token tiles)
 template <class DT, int NC, int NT, int WC, int WT, int DEPTH>
@@ -421,7 +423,10 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void dense_q8_small_kernel(DenseTa
 // The kernel for few tokens.  A workgroup computes 16 CH channels of up to 16 NT tokens; its WAVES waves divide k among
 // themselves in chunks of 128 bytes (a cache line of every row).  A wave's chunks go from memory to a ring of DEPTH places in
 // LDS that is its own, eight rows to a load, and from there to the matrix cores: no registers are held by what is in flight,
-// and no wave waits for another until their sums meet at the end.
+// and no wave waits for another until their sums meet at the end.  Wide blocks are for batches whose narrower ones would take a
+// second round of workgroups: 64 tokens, 5120 -> 2 x 13824 (128 channels, 216 workgroups) 35 us, with 32 to 96 channels 40 and more;
+// 8192 -> 28672 47 us (5.1 TB/s) against 53.  One token, 4096 -> 3 x 4096 12.0 us, 64 tokens, 4096 -> 2 x 11008 23 us (weights from
+// memory in all of these): what bounds them is memory and that a compute unit takes in some 40 bytes a nanosecond.
 // grid = (channel blocks of all projections, token blocks)
 template <int CH, int NT, int WAVES, int DEPTH>
 struct DenseFew {
@@ -650,7 +655,7 @@ constexpr DenseKernel few_of() {
 // In the order of launch_typed's cases.
 constexpr DenseKernel kKernels[] = {
     few_of<1, 1, 16, 2>(), few_of<2, 1, 8, 2>(), few_of<4, 1, 4, 2>(), few_of<2, 2, 8, 2>(), few_of<3, 2, 4, 2>(), few_of<2, 3, 4, 2>(),
-    few_of<6, 4, 4, 2>(),
+    few_of<6, 4, 4, 2>(), few_of<8, 4, 3, 2>(),
     tile_of<2, 1, 2, 2, 6>(0.26f, 0.22f, 1.27f),  // 64 x 32
     tile_of<2, 1, 2, 4, 6>(0.33f, 0.33f, 1.27f),  // 64 x 64
     tile_of<2, 2, 2, 4, 5>(0.47f, 0.50f, 1.27f),  // 64 x 128
@@ -659,7 +664,7 @@ constexpr DenseKernel kKernels[] = {
     tile_of<4, 4, 2, 4, 2>(1.08f, 1.10f, 1.15f),  // 128 x 256
     tile_of<8, 4, 2, 4, 2>(1.60f, 1.78f, 1.15f),  // 256 x 256
 };
-constexpr int kFewKernels = 7, kSmallKernels = 4;  // the rest are the large ones
+constexpr int kFewKernels = 8, kSmallKernels = 4;  // the rest are the large ones
 constexpr int kFewMostTokens = 128;
 
 template <class DT>
@@ -672,12 +677,13 @@ hipError_t launch_typed(const DenseArgs& a, const DensePlan& plan, hipStream_t s
     case 4: return launch_few<DT, 3, 2, 4, 2>(a, st);
     case 5: return launch_few<DT, 2, 3, 4, 2>(a, st);
     case 6: return launch_few<DT, 6, 4, 4, 2>(a, st);
-    case 7: return launch_small<DT, 2, 1, 2, 2, 6>(a, plan, st);
-    case 8: return launch_small<DT, 2, 1, 2, 4, 6>(a, plan, st);
-    case 9: return launch_small<DT, 2, 2, 2, 4, 5>(a, plan, st);
-    case 10: return launch_small<DT, 4, 2, 2, 4, 5>(a, plan, st);
-    case 11: return launch_large<DT, 4, 4, 2, 2, false>(a, plan, st);
-    case 12: return launch_large<DT, 4, 4, 2, 4, true>(a, plan, st);
+    case 7: return launch_few<DT, 8, 4, 3, 2>(a, st);
+    case 8: return launch_small<DT, 2, 1, 2, 2, 6>(a, plan, st);
+    case 9: return launch_small<DT, 2, 1, 2, 4, 6>(a, plan, st);
+    case 10: return launch_small<DT, 2, 2, 2, 4, 5>(a, plan, st);
+    case 11: return launch_small<DT, 4, 2, 2, 4, 5>(a, plan, st);
+    case 12: return launch_large<DT, 4, 4, 2, 2, false>(a, plan, st);
+    case 13: return launch_large<DT, 4, 4, 2, 4, true>(a, plan, st);
     default: return launch_large<DT, 8, 4, 2, 4, true>(a, plan, st);
   }
 }

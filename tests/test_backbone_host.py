@@ -139,7 +139,7 @@ def test_every_dense_kernel_is_reached_and_fits():
     # few tokens: rings of 80 K to 160 K; small tiles 64 x 32, 64 x 64, 64 x 128, 128 x 128; large 64 K, 96 K and 128 K
     assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_SMALL} == {72, 96, 120, 160}, seen
     assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_LARGE} == {64, 96, 128}, seen
-    assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_FEW} == {80, 96, 128, 160}, seen
+    assert {b >> 10 for k, b in seen if k == sg.KERNEL_DENSE_FEW} == {80, 96, 128, 144, 160}, seen
 
 
 def test_quantize_weight():

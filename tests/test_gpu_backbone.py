@@ -237,6 +237,8 @@ EVERY_KERNEL = [
     (1, 1152, (7208, 1024), 1, 9, 81920, 1),
     (33, 1280, (3568, 13200), 0, 9, 163840, 1),
     (68, 1160, (8320, 8), 1, 9, 163840, 1),
+    (33, 1280, (28672,), 0, 9, 147456, 1),
+    (64, 1160, (25000, 1032), 1, 9, 147456, 1),
     (2865, 1400, (264, 8), 0, 10, 122880, 1),
     (2897, 1152, (8, 280), 0, 10, 122880, 1),
     (2718, 11848, (8,), 1, 10, 122880, 8),
