@@ -395,7 +395,8 @@ int sgmv_plan_expand(const sgmv_problem* p, int32_t n_segs, sgmv_plan* plan);
  *   residual  device 16-bit [n_tokens][h] or NULL (s = x)
  *   weight    device 16-bit [h];  eps finite and not negative (else SGMV_ERR_UNSUPPORTED)
  * out may be x, or the residual, where sum is not.  The norm is taken of the fp32 s, not of the
- * rounded sum.  With eps 0 a row whose mean square is below fp32's range is not finite. */
+ * rounded sum; squares that leave fp32's range, above or below, are computed all the same.  With
+ * eps 0 a row of zeros is not finite. */
 int sgmv_rms_norm_q8(int32_t dtype, void* out, int8_t* q, float* q_scales, void* sum, const void* x,
                      const void* residual, const void* weight, float eps, int32_t n_tokens, int32_t h,
                      void* stream);

@@ -91,15 +91,17 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* x, const 
       return reduce_row(sum, of_waves, [](float a, float b) { return a + b; });
     };
     float sum = squares(sums[0]);
-    if ((__float_as_uint(sum) & 0x7FFFFFFFu) >= kInfBits) {
-      // values past about 1e18, whose squares leave fp32's range: the row times 2^-80, which the norm does not change by
-      // (what is not finite itself stays so)
-      constexpr float kDown = 0x1p-80f;
-      eps = eps * kDown * kDown;
+    const bool above = (__float_as_uint(sum) & 0x7FFFFFFFu) >= kInfBits;
+    if (above || sum * (1.0f / (float)h) + eps < 0x1p-100f) {
+      // Values past about 1e18, whose squares leave fp32's range: the row times 2^-80, which the norm does not change by (what
+      // is not finite itself stays so).  Values under about 1e-15 next to an eps that does not cover them: times 2^80, as squares
+      // lose bits from 2^-126 on (an error of 2^-150 each, nothing next to 2^-100), and are zero below 2^-150.
+      const float by = above ? 0x1p-80f : 0x1p80f;
+      eps = eps * by * by;
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] *= kDown;
+        for (int i = 0; i < 8; ++i) v[c][i] *= by;
       sum = squares(sums[1]);
     }
     const float inv = rsqrtf(sum * (1.0f / (float)h) + eps);
