@@ -433,7 +433,8 @@ int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* 
                   const int32_t* h_outs, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Host-only, pure: which kernel sgmv_dense_q8 would launch (`slices` = parts of the sum; with more than
- * one a second launch joins them).  Returns the status that the call's sizes alone give. */
+ * one a second launch joins them; batches with more output tiles than a launch takes are several
+ * launches of one kernel).  Returns the status that the call's sizes alone give. */
 int sgmv_plan_dense_q8(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, const int32_t* h_outs,
                        const void* workspace, size_t workspace_bytes, sgmv_plan* plan);
 

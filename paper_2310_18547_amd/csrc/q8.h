@@ -12,6 +12,8 @@ constexpr int kRowsMostWidth = 1024 * 4 * 8;
 constexpr int kDenseMostHin = 131064;
 // Most tokens, and widest output of a projection: rows and channels, all projections' together, are 32-bit numbers.
 constexpr int kDenseMostTokens = 1 << 30, kDenseMostHout = 1 << 27;
+// Most values of y in all: the workgroups of every kernel's tiles, padded to whole tiles of each projection, are a 32-bit number.
+constexpr long long kDenseMostValues = 1LL << 38;
 // Most projections of one sgmv_dense_q8 call.
 constexpr int kDenseMostProjections = 8;
 
@@ -49,11 +51,12 @@ struct DensePlan {
   int kernel;            // of q8_dense.hip's table
   DenseFamily family;
   int splits;            // workgroups that divide a tile's sum; from two on a second launch joins the parts
-  long long workgroups;
+  long long workgroups;  // of all launches
+  int tokens;            // of a launch, whole tiles; all of them but for batches beyond the threads of one launch
   int lds;               // bytes per workgroup
 };
-// The kernel for a call on a device of that many compute units; pure host arithmetic.  False: no launch takes it.
-bool plan_dense(const DenseArgs& a, int units, DensePlan* plan);
+// The kernel for a call on a device of that many compute units; pure host arithmetic.
+void plan_dense(const DenseArgs& a, int units, DensePlan* plan);
 hipError_t launch_dense(const DenseArgs& a, const DensePlan& plan, hipStream_t st);
 
 }  // namespace sgmv

@@ -34,10 +34,13 @@ int check_dense(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, c
   if (n_proj < 0 || n_proj > kDenseMostProjections || n_tokens < 0 || h_in <= 0) return SGMV_ERR_SHAPE;
   if (h_in % 8 != 0 || h_in > kDenseMostHin || n_tokens > kDenseMostTokens) return SGMV_ERR_UNSUPPORTED;
   if (n_proj > 0 && h_outs == nullptr) return SGMV_ERR_NULL;
+  long long channels = 0;
   for (int i = 0; i < n_proj; ++i) {
     if (h_outs[i] <= 0) return SGMV_ERR_SHAPE;
     if (h_outs[i] % 8 != 0 || h_outs[i] > kDenseMostHout) return SGMV_ERR_UNSUPPORTED;
+    channels += h_outs[i];
   }
+  if (n_tokens * channels > kDenseMostValues) return SGMV_ERR_UNSUPPORTED;
   return aligned(workspace, 256) ? SGMV_OK : SGMV_ERR_ALIGN;
 }
 
@@ -120,7 +123,7 @@ int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* 
     a.y[i] = ys[i];
   }
   DensePlan plan;
-  if (!plan_dense(a, compute_units(), &plan)) return SGMV_ERR_UNSUPPORTED;
+  plan_dense(a, compute_units(), &plan);
   return launch_dense(a, plan, static_cast<hipStream_t>(stream)) == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
 }
 
@@ -132,10 +135,9 @@ int sgmv_plan_dense_q8(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t 
   const int rc = check_dense(dtype, n_proj, n_tokens, h_in, h_outs, workspace, &nothing);
   if (rc != SGMV_OK || nothing) return rc;
   DensePlan d;
-  if (!plan_dense(dense_shape(dtype, n_proj, n_tokens, h_in, h_outs, const_cast<void*>(workspace), workspace_bytes), compute_units(), &d))
-    return SGMV_ERR_UNSUPPORTED;
+  plan_dense(dense_shape(dtype, n_proj, n_tokens, h_in, h_outs, const_cast<void*>(workspace), workspace_bytes), compute_units(), &d);
   plan->kernel = d.family == kDenseFew ? SGMV_KERNEL_DENSE_FEW : d.family == kDenseSmall ? SGMV_KERNEL_DENSE_SMALL : SGMV_KERNEL_DENSE_LARGE;
-  plan->launches = d.splits > 1 ? 2 : 1;
+  plan->launches = d.splits > 1 ? 2 : (n_tokens + d.tokens - 1LL) / d.tokens;
   plan->slices = d.splits;
   plan->workgroups = (int32_t)d.workgroups;
   plan->lds_bytes = d.lds;

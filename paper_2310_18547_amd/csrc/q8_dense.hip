@@ -600,7 +600,7 @@ hipError_t launch_tiles(Kernel kernel, std::atomic<bool>* allowed, const DenseAr
   const DenseTable t = fill_table(a, T::kChannels);
   const DenseShape shape = {a.n_tokens, a.h_in, a.n_proj, ceil_div(a.n_tokens, T::kTokens), plan.splits,
                             t.before[a.n_proj - 1] + a.h_out[a.n_proj - 1], static_cast<int*>(a.workspace)};
-  kernel<<<(unsigned)plan.workgroups, T::kThreads, T::kLds, st>>>(t, a.q, a.q_scales, shape);
+  kernel<<<(unsigned)(t.first[a.n_proj] * shape.token_tiles * plan.splits), T::kThreads, T::kLds, st>>>(t, a.q, a.q_scales, shape);
   const hipError_t launched = hipGetLastError();
   if (launched != hipSuccess || plan.splits == 1) return launched;
   const dim3 grid((unsigned)ceil_div(shape.all_channels, 8 * 256), (unsigned)a.n_tokens);
@@ -690,57 +690,70 @@ hipError_t launch_typed(const DenseArgs& a, const DensePlan& plan, hipStream_t s
 
 }  // namespace
 
-bool plan_dense(const DenseArgs& a, int units, DensePlan* plan) {
+void plan_dense(const DenseArgs& a, int units, DensePlan* plan) {
+  constexpr long long kMostThreads = 0xFFFFFFFFLL;  // of a launch
   double weights = 0.0, channels = 0.0;  // bytes of w; channels of all projections
   for (int i = 0; i < a.n_proj; ++i) channels += a.h_out[i];
   weights = channels * a.h_in;
   const int all = a.h_in / 128;  // whole steps
   double best = 0.0;
   plan->kernel = -1;
-  for (int k = 0; k < (int)(sizeof kKernels / sizeof kKernels[0]); ++k) {
-    const DenseKernel& kernel = kKernels[k];
-    const bool few = k < kFewKernels;
-    if (few && a.n_tokens > kFewMostTokens) continue;
-    long long blocks = 0;
-    for (int i = 0; i < a.n_proj; ++i) blocks += ceil_div(a.h_out[i], kernel.channels);
-    const long long token_blocks = ceil_div(a.n_tokens, kernel.tokens);
-    if (blocks > 0x7FFFFFFF / token_blocks) continue;
-    for (int splits = 1; splits <= 8; ++splits) {
-      if (splits > 1) {
-        // parts of eight steps and more, 16 bytes of partial sums written and read per value and part
-        if (few || all < 8 * splits || a.n_tokens > 65535 || 4.0 * splits * a.n_tokens * channels > (double)a.workspace_bytes) break;
-      }
-      const long long groups = blocks * token_blocks * splits;
-      if (groups * kernel.threads > 0xFFFFFFFFLL) break;  // threads of a launch
-      const double rounds = (double)((groups + units - 1) / units), askew = a.h_in % 128 != 0 ? kernel.askew : 1.0;
-      double us;
-      if (few) {
-        const double unit = askew * rounds * (kernel.channels + kernel.tokens) * a.h_in / 40e3;
-        // weights that later token blocks read again come from the cache behind the L2s
-        const double memory = weights * (1.0 + 0.2 * (double)(token_blocks - 1)) / 5.4e6;
-        us = unit > memory ? unit : memory;
-        if (kernel.threads > 512 && rounds > 1.0) us *= 1.1;  // sixteen waves only where one workgroup to a unit is all there is
-      } else {
-        const double steps = (double)ceil_div(all, splits) + (a.h_in % 128 != 0);
-        const double unit = askew * steps * (rounds > 1.0 ? rounds * kernel.more : kernel.one), memory = weights / 5.0e6;
-        us = unit > memory ? unit : memory;
-        if (splits > 1) us += 3.0 + 8.0 * splits * a.n_tokens * channels / 4e6;  // the second launch
-      }
-      if (plan->kernel < 0 || us < best) {
-        best = us;
-        plan->kernel = k;
-        plan->family = few ? kDenseFew : k < kFewKernels + kSmallKernels ? kDenseSmall : kDenseLarge;
-        plan->splits = splits;
-        plan->workgroups = groups;
-        plan->lds = kernel.lds;
+  // One launch; where no kernel's threads fit into one, the tokens in ranges, a launch each.  A token block of the largest tiles
+  // fits into a launch whatever the number of channels, so there is always a choice.
+  for (int ranges = 0; ranges < 2 && plan->kernel < 0; ++ranges)
+    for (int k = 0; k < (int)(sizeof kKernels / sizeof kKernels[0]); ++k) {
+      const DenseKernel& kernel = kKernels[k];
+      const bool few = k < kFewKernels;
+      if (few && a.n_tokens > kFewMostTokens) continue;
+      long long blocks = 0;
+      for (int i = 0; i < a.n_proj; ++i) blocks += ceil_div(a.h_out[i], kernel.channels);
+      const long long token_blocks = ceil_div(a.n_tokens, kernel.tokens), range = kMostThreads / (blocks * kernel.threads);
+      if (ranges == 0 ? token_blocks > range : range == 0) continue;
+      for (int splits = 1; splits <= 8; ++splits) {
+        if (splits > 1) {
+          // parts of eight steps and more, 4 bytes of partial sums written and read per value and part
+          if (few || all < 8 * splits || a.n_tokens > 65535 || 4.0 * splits * a.n_tokens * channels > (double)a.workspace_bytes) break;
+          if (token_blocks * splits > range) break;
+        }
+        const long long groups = blocks * token_blocks * splits;
+        const double rounds = (double)((groups + units - 1) / units), askew = a.h_in % 128 != 0 ? kernel.askew : 1.0;
+        double us;
+        if (few) {
+          const double unit = askew * rounds * (kernel.channels + kernel.tokens) * a.h_in / 40e3;
+          // weights that later token blocks read again come from the cache behind the L2s
+          const double memory = weights * (1.0 + 0.2 * (double)(token_blocks - 1)) / 5.4e6;
+          us = unit > memory ? unit : memory;
+          if (kernel.threads > 512 && rounds > 1.0) us *= 1.1;  // sixteen waves only where one workgroup to a unit is all there is
+        } else {
+          const double steps = (double)ceil_div(all, splits) + (a.h_in % 128 != 0);
+          const double unit = askew * steps * (rounds > 1.0 ? rounds * kernel.more : kernel.one), memory = weights / 5.0e6;
+          us = unit > memory ? unit : memory;
+          if (splits > 1) us += 3.0 + 8.0 * splits * a.n_tokens * channels / 4e6;  // the second launch
+        }
+        if (plan->kernel < 0 || us < best) {
+          best = us;
+          plan->kernel = k;
+          plan->family = few ? kDenseFew : k < kFewKernels + kSmallKernels ? kDenseSmall : kDenseLarge;
+          plan->splits = splits;
+          plan->workgroups = groups;
+          plan->lds = kernel.lds;
+          plan->tokens = token_blocks > range ? (int)range * kernel.tokens : a.n_tokens;
+        }
       }
     }
-  }
-  return plan->kernel >= 0;
 }
 
 hipError_t launch_dense(const DenseArgs& a, const DensePlan& plan, hipStream_t st) {
-  return a.bf16 ? launch_typed<BF16>(a, plan, st) : launch_typed<F16>(a, plan, st);
+  DenseArgs part = a;
+  for (int first = 0; first < a.n_tokens; first += part.n_tokens) {
+    part.n_tokens = a.n_tokens - first < plan.tokens ? a.n_tokens - first : plan.tokens;
+    part.q = a.q + (size_t)first * a.h_in;
+    part.q_scales = a.q_scales + first;
+    for (int i = 0; i < a.n_proj; ++i) part.y[i] = static_cast<uint16_t*>(a.y[i]) + (size_t)first * a.h_out[i];
+    const hipError_t err = a.bf16 ? launch_typed<BF16>(part, plan, st) : launch_typed<F16>(part, plan, st);
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 }  // namespace sgmv

@@ -1,6 +1,7 @@
 """Edges of the 8-bit backbone calls on the GPU: sums of a few steps in every dense kernel, norms of the smallest rows."""
 import numpy as np
 import pytest
+import torch
 
 import backbone_reference as ref
 from test_gpu_backbone import KIND, Q8, _behind, _bits, _dense_inputs, _dev, _host, _marked
@@ -158,3 +159,31 @@ def test_norm_of_rows_whose_squares_leave_fp32(eps, h):
         assert np.all(np.isfinite(exact))
         q, scales = q8.get()
         ref.check_rows(exact, _host(out)[:n], q, scales, "bf16", (eps, h))
+
+
+def test_dense_of_more_tiles_than_a_launch_takes():
+    """Several launches over ranges of tokens, every row of every projection against the whole sums."""
+    from paper_2310_18547_amd import binding as B
+    n, h_in, h_out, projections = (1 << 28) + 300, 8, 8, 8
+    assert B.sgmv_plan_dense_q8(B.BF16, n, h_in, [h_out] * projections).launches > 1
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    period = (1 << 20) + 7                          # odd: equal rows lie differently in every tile and launch
+    some = torch.randint(-128, 128, (period, h_in), generator=gen, dtype=torch.int8, device="cuda:0")
+    some_scales = torch.rand(period, generator=gen, device="cuda:0") + 0.01
+    q = torch.empty(n, h_in, dtype=torch.int8, device="cuda:0")
+    q_scales = torch.empty(n, device="cuda:0")
+    for lo in range(0, n, period):
+        rows = min(period, n - lo)
+        q[lo:lo + rows], q_scales[lo:lo + rows] = some[:rows], some_scales[:rows]
+    ws = [torch.randint(-128, 128, (h_out, h_in), generator=gen, dtype=torch.int8, device="cuda:0") for _ in range(projections)]
+    w_scales = [torch.rand(h_out, generator=gen, device="cuda:0") + 0.01 for _ in range(projections)]
+    ys = [torch.full((n + 2, h_out), 7.0, dtype=torch.bfloat16, device="cuda:0") for _ in range(projections)]
+    B.sgmv_dense_q8(B.BF16, ys, q, q_scales, ws, w_scales, n, h_in, [h_out] * projections)
+    for y, w, s in zip(ys, ws, w_scales):
+        # whole sums below 2^18 are exact in fp32 in any order; then the scales one after the other and one rounding
+        want = (((some.float()[:, None, :] * w.float()[None]).sum(2) * some_scales[:, None]) * s).to(torch.bfloat16)
+        for lo in range(0, n, period):
+            rows = min(period, n - lo)
+            same = torch.equal(y[lo:lo + rows], want[:rows])
+            assert same, lo
+        assert torch.all(y[n:] == 7.0)
