@@ -384,7 +384,8 @@ int sgmv_plan_expand(const sgmv_problem* p, int32_t n_segs, sgmv_plan* plan);
  *   - 16-bit rows and 8-bit rows are 16-byte aligned, q_scales 4-byte, w_scales and weights
  *     16-byte (else SGMV_ERR_ALIGN); widths are positive multiples of 8, in the row calls at most
  *     32768 (else SGMV_ERR_UNSUPPORTED).  n_tokens == 0 returns SGMV_OK and enqueues nothing.
- *   - Buffers that a call writes must not overlap one another or what it reads, except where said.
+ *   - Buffers that a call writes must not overlap one another or what it reads, except where said:
+ *     SGMV_ERR_SHAPE (of a workspace, where the call would leave partial sums).
  *   - Calls are asynchronous on `stream`, which belongs to the current device, like the buffers. */
 
 /* Root-mean-square norm with the residual's addition:
@@ -414,7 +415,7 @@ int sgmv_quantize_q8(int32_t dtype, int8_t* q, float* q_scales, const void* x, i
  *   y_i[t][c] = (sum_j q[t][j] * w_i[c][j]) * q_scales[t] * w_scales_i[c],   i < n_proj <= 8
  * The sum is an exact 32-bit integer, scaled in fp32 and rounded once when y is stored (y is
  * written, not accumulated into).
- *   ys        HOST array of device pointers, y_i 16-bit [n_tokens][h_outs[i]], distinct
+ *   ys        HOST array of device pointers, y_i 16-bit [n_tokens][h_outs[i]]
  *   q, q_scales  device, as above, width h_in, at most 131064; any int8 values (-128 too)
  *   ws        HOST array of device pointers, w_i int8 [h_outs[i]][h_in] (an output channel's weights
  *             in a row)

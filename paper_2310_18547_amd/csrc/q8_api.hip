@@ -12,6 +12,16 @@ using namespace sgmv;
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// A device buffer of a call; none at all where `at` is nullptr.
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+inline bool overlap(const Span& a, const Span& b) {
+  const uintptr_t from = reinterpret_cast<uintptr_t>(a.at), to = reinterpret_cast<uintptr_t>(b.at);
+  return a.at != nullptr && b.at != nullptr && (to - from < a.bytes || from - to < b.bytes);
+}
+
 int check_rows(int32_t dtype, int32_t n_tokens, int32_t h) {
   if (dtype != SGMV_F16 && dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
   if (n_tokens < 0 || h <= 0) return SGMV_ERR_SHAPE;
@@ -24,6 +34,39 @@ int check_q8(const int8_t* q, const float* q_scales, bool must) {
   if ((q == nullptr) != (q_scales == nullptr) || (must && q == nullptr)) return SGMV_ERR_NULL;
   if (!aligned(q, 16) || !aligned(q_scales, 4)) return SGMV_ERR_ALIGN;
   return SGMV_OK;
+}
+
+// Whether a row call would overwrite what it still reads, or one of its outputs another.  A thread reads its part of every input
+// before it stores, so a 16-bit output may be an input as a whole; 8-bit rows lie elsewhere than the 16-bit ones they come from.
+bool rows_overlap(const RowsArgs& a) {
+  const size_t n = (size_t)a.n_tokens, values = n * (size_t)a.h;
+  const Span written[] = {{a.out, 2 * values}, {a.sum, 2 * values}, {a.q, values}, {a.q_scales, 4 * n}};
+  const Span read[] = {{a.x, 2 * values}, {a.other, 2 * values}, {a.weight, 2 * (size_t)a.h}};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (overlap(written[i], written[j])) return true;
+    for (int j = 0; j < 3; ++j)
+      if (overlap(written[i], read[j]) && !(i < 2 && j < 2 && written[i].at == read[j].at)) return true;
+  }
+  return false;
+}
+
+// The same of a dense call with that many bytes of partial sums.
+bool dense_overlap(const DenseArgs& a, size_t partials) {
+  const size_t n = (size_t)a.n_tokens, h_in = (size_t)a.h_in;
+  const Span q = {a.q, n * h_in}, q_scales = {a.q_scales, 4 * n}, scratch = {partials > 0 ? a.workspace : nullptr, partials};
+  if (overlap(scratch, q) || overlap(scratch, q_scales)) return true;
+  for (int i = 0; i < a.n_proj; ++i) {
+    const size_t channels = (size_t)a.h_out[i];
+    const Span y = {a.y[i], 2 * n * channels}, w = {a.w[i], channels * h_in}, w_scales = {a.w_scales[i], 4 * channels};
+    if (overlap(y, q) || overlap(y, q_scales) || overlap(y, scratch) || overlap(scratch, w) || overlap(scratch, w_scales)) return true;
+    for (int j = 0; j < a.n_proj; ++j) {
+      const size_t others = (size_t)a.h_out[j];
+      if (overlap(y, {a.w[j], others * h_in}) || overlap(y, {a.w_scales[j], 4 * others})) return true;
+      if (j < i && overlap(y, {a.y[j], 2 * n * others})) return true;
+    }
+  }
+  return false;
 }
 
 // What a dense call and its plan refuse alike; `*nothing`: the call has nothing to do.
@@ -58,6 +101,7 @@ DenseArgs dense_shape(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h
 }
 
 int launch(const RowsArgs& a, void* stream) {
+  if (rows_overlap(a)) return SGMV_ERR_SHAPE;
   return launch_rows(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
 }
 
@@ -75,7 +119,6 @@ int sgmv_rms_norm_q8(int32_t dtype, void* out, int8_t* q, float* q_scales, void*
   rc = check_q8(q, q_scales, false);
   if (rc != SGMV_OK) return rc;
   if (!aligned(out, 16) || !aligned(sum, 16) || !aligned(x, 16) || !aligned(residual, 16) || !aligned(weight, 16)) return SGMV_ERR_ALIGN;
-  if ((out != nullptr && (out == sum || out == weight)) || sum == weight) return SGMV_ERR_SHAPE;  // one would be lost
   return launch(RowsArgs{kRowsNorm, dtype == SGMV_BF16, n_tokens, h, eps, x, residual, weight, sum, out, q, q_scales}, stream);
 }
 
@@ -116,14 +159,15 @@ int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* 
   for (int i = 0; i < n_proj; ++i) {
     if (ys[i] == nullptr || ws[i] == nullptr || w_scales[i] == nullptr) return SGMV_ERR_NULL;
     if (!aligned(ys[i], 16) || !aligned(ws[i], 16) || !aligned(w_scales[i], 16)) return SGMV_ERR_ALIGN;
-    for (int j = 0; j < i; ++j)
-      if (ys[i] == ys[j]) return SGMV_ERR_SHAPE;  // two projections into one y would race
     a.w[i] = ws[i];
     a.w_scales[i] = w_scales[i];
     a.y[i] = ys[i];
   }
   DensePlan plan;
   plan_dense(a, compute_units(), &plan);
+  size_t channels = 0;
+  for (int i = 0; i < n_proj; ++i) channels += (size_t)h_outs[i];
+  if (dense_overlap(a, plan.splits > 1 ? 4 * channels * n_tokens * plan.splits : 0)) return SGMV_ERR_SHAPE;
   return launch_dense(a, plan, static_cast<hipStream_t>(stream)) == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
 }
 
