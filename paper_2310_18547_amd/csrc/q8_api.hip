@@ -71,10 +71,11 @@ bool dense_overlap(const DenseArgs& a, size_t partials) {
 
 // What a dense call and its plan refuse alike; `*nothing`: the call has nothing to do.
 int check_dense(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, const int32_t* h_outs, const void* workspace,
-                bool* nothing) {
+                size_t workspace_bytes, bool* nothing) {
   *nothing = n_proj == 0 || n_tokens == 0;
   if (dtype != SGMV_F16 && dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
   if (n_proj < 0 || n_proj > kDenseMostProjections || n_tokens < 0 || h_in <= 0) return SGMV_ERR_SHAPE;
+  if (workspace_bytes > SIZE_MAX / 2) return SGMV_ERR_SHAPE;  // a negative number of the caller's
   if (h_in % 8 != 0 || h_in > kDenseMostHin || n_tokens > kDenseMostTokens) return SGMV_ERR_UNSUPPORTED;
   if (n_proj > 0 && h_outs == nullptr) return SGMV_ERR_NULL;
   long long channels = 0;
@@ -149,7 +150,7 @@ int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* 
                   const float* const* w_scales, int32_t n_tokens, int32_t h_in, const int32_t* h_outs, void* workspace,
                   size_t workspace_bytes, void* stream) {
   bool nothing = false;
-  const int rc = check_dense(dtype, n_proj, n_tokens, h_in, h_outs, workspace, &nothing);
+  const int rc = check_dense(dtype, n_proj, n_tokens, h_in, h_outs, workspace, workspace_bytes, &nothing);
   if (rc != SGMV_OK || nothing) return rc;
   if (ys == nullptr || q == nullptr || q_scales == nullptr || ws == nullptr || w_scales == nullptr) return SGMV_ERR_NULL;
   if (!aligned(q, 16) || !aligned(q_scales, 4)) return SGMV_ERR_ALIGN;
@@ -176,7 +177,7 @@ int sgmv_plan_dense_q8(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t 
   if (plan == nullptr) return SGMV_ERR_NULL;
   *plan = sgmv_plan{};
   bool nothing = false;
-  const int rc = check_dense(dtype, n_proj, n_tokens, h_in, h_outs, workspace, &nothing);
+  const int rc = check_dense(dtype, n_proj, n_tokens, h_in, h_outs, workspace, workspace_bytes, &nothing);
   if (rc != SGMV_OK || nothing) return rc;
   DensePlan d;
   plan_dense(dense_shape(dtype, n_proj, n_tokens, h_in, h_outs, const_cast<void*>(workspace), workspace_bytes), compute_units(), &d);

@@ -94,3 +94,10 @@ def test_dense_refuses_partial_sums_over_its_buffers():
             p = list(far)
             p[i] = at
             assert _dense([p[0]], p[1], p[2], [p[3]], [p[4]], scratch, 16 << 20, n, h_in, h_outs) == SHAPE, (i, at - scratch)
+
+
+def test_dense_refuses_a_negative_workspace_size():
+    """As an unsigned number it would be room for any partial sums."""
+    for nbytes in (-1, -(1 << 40)):
+        assert sg.sgmv_plan_dense_q8(sg.F16, 100, 8192, [1032], 1 << 32, nbytes, check=False)[0] == SHAPE
+        assert _dense([2 << 32], 3 << 32, 4 << 32, [5 << 32], [6 << 32], 1 << 32, nbytes, 100, 8192, [1032]) == SHAPE
