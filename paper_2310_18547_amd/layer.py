@@ -75,11 +75,32 @@ def quantize_weight(w: torch.Tensor):
     return torch.round(w.float() / scales).clamp(-127, 127).to(torch.int8).contiguous(), scales[:, 0].contiguous()
 
 
+def _require(t, kind, rows: int, width: int, device, what: str, exactly: bool = False) -> None:
+    """Raises ``ValueError`` unless ``t`` holds ``rows`` rows or more of ``width`` values (one or several last dimensions together)
+    without gaps; ``exactly``: is ``[rows, width]`` itself.  Its address is all that a call gets: anything else would be read as
+    something else, or past its end.  An ``int`` is an address that the caller answers for."""
+    if isinstance(t, int) and not exactly:
+        return
+    got = f"{type(t)!r}"
+    if isinstance(t, torch.Tensor):
+        values = 1
+        for n in reversed(t.shape):
+            values *= n
+            if values >= width:
+                break
+        fits = tuple(t.shape) == (rows, width) if exactly else values == width and t.numel() >= rows * width
+        if fits and t.dtype == kind and t.device == device and t.is_contiguous():
+            return
+        got = f"{tuple(t.shape)} of {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}"
+    raise ValueError(f"{what}: {rows} contiguous rows of {width} {kind} on {device}, not {got}")
+
+
 class Q8Layer(LoraLayer):
     """A decoder layer with an 8-bit backbone and 16-bit LoRA add-ons, for batches of ``n_tokens`` rows.
 
     ``weights`` holds, for every name of ``PROJECTIONS``, a list with a layer's ``(int8 [h_out, h_in], fp32 [h_out])`` for every
-    layer; ``norms`` the 16-bit norm weights of every layer, ``(in front of attention, in front of the MLP)``.  The
+    layer; ``norms`` the 16-bit norm weights of every layer, ``(in front of attention, in front of the MLP)``.  Tensors
+    of another type, shape, layout or device raise ``ValueError``.  The
     buffers are the object's own and are used again by the next call: one call at a time, on one stream.
     """
 
@@ -89,11 +110,19 @@ class Q8Layer(LoraLayer):
         self.dtype, self.n_tokens, self.h, self.ffn, self.eps = dtype, n_tokens, h, ffn, eps
         self.weights, self.norms = weights, norms
         self.add_ons = True  # False: the backbone alone (benchmarks compare the two)
+        self.kind = kind = torch.float16 if dtype == B.F16 else torch.bfloat16
+        on = self.workspace.device
         for name, (h_in, h_out) in self.shapes.items():
+            if len(weights[name]) < num_layers:
+                raise ValueError(f"{name}: weights of {len(weights[name])} layers, not {num_layers}")
             for w, s in weights[name]:
-                assert w.dtype == torch.int8 and w.shape == (h_out, h_in) and w.is_contiguous(), name
-                assert s.dtype == torch.float32 and s.shape == (h_out,) and s.is_contiguous(), name
-        kind = torch.float16 if dtype == B.F16 else torch.bfloat16
+                _require(w, torch.int8, h_out, h_in, on, f"weight of {name}", exactly=True)
+                _require(s[None], torch.float32, 1, h_out, on, f"weight scales of {name}", exactly=True)
+        if len(norms) < num_layers:
+            raise ValueError(f"norm weights of {len(norms)} layers, not {num_layers}")
+        for pair in norms:
+            for w in pair:
+                _require(w, kind, 1, h, on, "norm weight")
 
         def rows(width, kind=kind):
             return torch.empty(n_tokens, width, dtype=kind, device=device)
@@ -103,9 +132,18 @@ class Q8Layer(LoraLayer):
         self.q, self.q_ffn = rows(h, torch.int8), rows(ffn, torch.int8)  # in 8 bits
         self.q_scales = torch.empty(n_tokens, dtype=torch.float32, device=device)
         self.scratch = torch.empty(B.DENSE_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+        self._own = {id(t): (t, t.shape[1], t.dtype) for t in (*self.y.values(), self.x, self.act, self.q, self.q_ffn)}
+
+    def _rows(self, t, width: int, what: str, kind=None) -> None:
+        """Checks a caller's rows; the object's own buffers are known."""
+        kind = kind or self.kind
+        own = self._own.get(id(t))
+        if own is None or own[1:] != (width, kind):
+            _require(t, kind, self.n_tokens, width, self.x.device, what)
 
     def dense(self, names: Sequence[str], q, layer_idx: int, stream=None) -> None:
         """Projections of the same 8-bit rows into ``self.y``, without their add-ons."""
+        self._rows(q, self.shapes[names[0]][0], "q", torch.int8)
         pairs = [self.weights[n][layer_idx] for n in names]
         B.sgmv_dense_q8(self.dtype, [self.y[n] for n in names], q, self.q_scales, [w for w, _ in pairs], [s for _, s in pairs],
                         self.n_tokens, self.shapes[names[0]][0], [self.shapes[n][1] for n in names], self.scratch,
@@ -113,6 +151,8 @@ class Q8Layer(LoraLayer):
 
     def project(self, names: Sequence[str], q, x, layer_idx: int, scale: float = 1.0, stream=None) -> None:
         """Projections of the same rows, ``q`` in 8 bits and ``x`` in 16, and their add-ons, into ``self.y``."""
+        if self.add_ons:
+            self._rows(x, self.shapes[names[0]][0], "x")
         self.dense(names, q, layer_idx, stream)
         if self.add_ons:
             self.add_lora_group(names, [self.y[n] for n in names], [x] * len(names), layer_idx, scale, stream)
@@ -120,6 +160,9 @@ class Q8Layer(LoraLayer):
     def norm(self, which: int, x, residual, layer_idx: int, stream=None) -> None:
         """``residual += x`` (in place), its norm into ``self.x`` and ``self.q``; ``which``: 0 attention's, 1 the MLP's.  ``x`` None:
         the residual as it is."""
+        for t, what in ((x, "x"), (residual, "residual")):
+            if t is not None:
+                self._rows(t, self.h, what)
         s = residual if x is None else x
         B.sgmv_rms_norm_q8(self.dtype, self.x, self.q, self.q_scales, None if x is None else residual, s,
                            None if x is None else residual, self.norms[layer_idx][which], self.eps, self.n_tokens, self.h, stream)
@@ -132,6 +175,9 @@ class Q8Layer(LoraLayer):
 
     def finish(self, attention, residual, layer_idx: int, scale: float = 1.0, stream=None):
         """From attention's output on: o, norm, gate / up, activation, down.  Returns what the next layer adds to the residual."""
+        self._rows(attention, self.h, "attention")
+        if residual is not None:
+            self._rows(residual, self.h, "residual")  # before anything is enqueued
         B.sgmv_quantize_q8(self.dtype, self.q, self.q_scales, attention, self.n_tokens, self.h, stream)
         self.project(("o",), self.q, attention, layer_idx, scale, stream)
         self.norm(1, self.y["o"], residual, layer_idx, stream)
