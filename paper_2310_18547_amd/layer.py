@@ -100,8 +100,9 @@ class Q8Layer(LoraLayer):
 
     ``weights`` holds, for every name of ``PROJECTIONS``, a list with a layer's ``(int8 [h_out, h_in], fp32 [h_out])`` for every
     layer; ``norms`` the 16-bit norm weights of every layer, ``(in front of attention, in front of the MLP)``.  Tensors
-    of another type, shape, layout or device raise ``ValueError``.  The
-    buffers are the object's own and are used again by the next call: one call at a time, on one stream.
+    of another type, shape, layout or device raise ``ValueError``, and so do rows in a buffer of the object that the call writes
+    before it last reads them.  The buffers are the object's own and are used again by the next call: one call at a time, on one
+    stream.
     """
 
     def __init__(self, h: int, ffn: int, r: int, num_layers: int, n_tokens: int, dtype: int, A_ptrs, B_ptrs, seg_starts,
@@ -141,6 +142,11 @@ class Q8Layer(LoraLayer):
         if own is None or own[1:] != (width, kind):
             _require(t, kind, self.n_tokens, width, self.x.device, what)
 
+    def _apart(self, t, buffers, what: str) -> None:
+        """Refuses a tensor in one of the object's own buffers that the call writes before it last reads the tensor."""
+        if isinstance(t, torch.Tensor) and t.numel() and t.untyped_storage().data_ptr() in [b.untyped_storage().data_ptr() for b in buffers]:
+            raise ValueError(f"{what} lies in a buffer of the layer that this call writes")
+
     def dense(self, names: Sequence[str], q, layer_idx: int, stream=None) -> None:
         """Projections of the same 8-bit rows into ``self.y``, without their add-ons."""
         self._rows(q, self.shapes[names[0]][0], "q", torch.int8)
@@ -153,6 +159,7 @@ class Q8Layer(LoraLayer):
         """Projections of the same rows, ``q`` in 8 bits and ``x`` in 16, and their add-ons, into ``self.y``."""
         if self.add_ons:
             self._rows(x, self.shapes[names[0]][0], "x")
+            self._apart(x, [self.y[n] for n in names], "x")  # the add-ons read it after the projections are written
         self.dense(names, q, layer_idx, stream)
         if self.add_ons:
             self.add_lora_group(names, [self.y[n] for n in names], [x] * len(names), layer_idx, scale, stream)
@@ -169,6 +176,7 @@ class Q8Layer(LoraLayer):
 
     def qkv(self, x, residual, layer_idx: int, scale: float = 1.0, stream=None):
         """Up to attention: norm, q / k / v with their add-ons."""
+        self._apart(residual, (self.x, self.y["q"], self.y["k"], self.y["v"]), "residual")
         self.norm(0, x, residual, layer_idx, stream)
         self.project(("q", "k", "v"), self.q, self.x, layer_idx, scale, stream)
         return self.y["q"], self.y["k"], self.y["v"]
@@ -178,6 +186,9 @@ class Q8Layer(LoraLayer):
         self._rows(attention, self.h, "attention")
         if residual is not None:
             self._rows(residual, self.h, "residual")  # before anything is enqueued
+            self._apart(residual, (self.y["o"], self.x, self.y["gate"], self.y["up"], self.act, self.y["down"]), "residual")
+        if self.add_ons:
+            self._apart(attention, (self.y["o"],), "attention")
         B.sgmv_quantize_q8(self.dtype, self.q, self.q_scales, attention, self.n_tokens, self.h, stream)
         self.project(("o",), self.q, attention, layer_idx, scale, stream)
         self.norm(1, self.y["o"], residual, layer_idx, stream)

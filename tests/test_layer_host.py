@@ -29,9 +29,9 @@ def _norms():
     return [(torch.ones(H, dtype=KIND), torch.ones(H, dtype=KIND)) for _ in range(LAYERS)]
 
 
-def _layer(weights=None, norms=None):
+def _layer(weights=None, norms=None, n=N):
     pointers = {name: torch.zeros(1, dtype=torch.int64) for name in PROJECTIONS}
-    return Q8Layer(H, FFN, 8, LAYERS, N, sg.F16, pointers, pointers, torch.tensor([0, N], dtype=torch.int32), 1, N,
+    return Q8Layer(H, FFN, 8, LAYERS, n, sg.F16, pointers, pointers, torch.tensor([0, n], dtype=torch.int32), 1, n,
                    weights or _weights(), norms or _norms(), device="cpu")
 
 
@@ -113,3 +113,28 @@ def test_weights_and_norms_that_are_not_the_layers(calls):
         with pytest.raises(ValueError, match="norm weight"):
             _layer(norms=[_norms()[0], (_norms()[1][0], bad)])
     _layer(norms=[tuple(w[None] for w in pair) for pair in _norms()])
+
+
+def test_rows_in_buffers_that_the_call_overwrites_first(calls):
+    """Attention in o's output is gone when o's add-on reads it, a residual in any buffer of a later stage when it is returned."""
+    t = _layer()
+    for call in (lambda: t.finish(t.y["o"], _rows(), 0), lambda: t.finish(t.y["o"].view(N, 4, H // 4), _rows(), 0),
+                 lambda: t.project(("o",), t.q, t.y["o"], 0), lambda: t.project(("q", "k", "v"), t.q, t.y["v"], 0),
+                 lambda: t.finish(_rows(), t.y["down"], 0), lambda: t.finish(_rows(), t.y["o"], 0), lambda: t.finish(_rows(), t.x, 0),
+                 lambda: t.qkv(None, t.x, 0), lambda: t.qkv(_rows(), t.y["q"], 0)):
+        with pytest.raises(ValueError, match="this call writes"):
+            call()
+        assert not calls
+    t.qkv(t.y["down"], _rows(), 0)                # read before anything of it is written
+    t.qkv(t.x, _rows(), 0)
+    t.qkv(None, t.y["down"], 0)
+    t.finish(t.x, _rows(), 0)
+    t.finish(t.y["q"], t.y["k"], 0)
+    t.add_ons = False
+    t.finish(t.y["o"], _rows(), 0)                # in 8 bits before o is written, and read by nothing else
+
+
+def test_a_batch_without_rows(calls):
+    t = _layer(n=0)
+    t.qkv(_rows(0), _rows(0), 0)
+    t.finish(t.y["v"], _rows(0), 0)
