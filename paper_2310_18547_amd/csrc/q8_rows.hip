@@ -90,21 +90,20 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(const uint16_t* x, const 
         for (int i = 0; i < 8; ++i) sum += v[c][i] * v[c][i];
       return reduce_row(sum, of_waves, [](float a, float b) { return a + b; });
     };
-    float sum = squares(sums[0]);
-    const bool above = (__float_as_uint(sum) & 0x7FFFFFFFu) >= kInfBits;
-    if (above || sum * (1.0f / (float)h) + eps < 0x1p-100f) {
+    const float per = 1.0f / (float)h;
+    float mean = squares(sums[0]) * per + eps;
+    if (!(mean >= 0x1p-100f && mean < __uint_as_float(kInfBits))) {
       // Values past about 1e18, whose squares leave fp32's range: the row times 2^-80, which the norm does not change by (what
       // is not finite itself stays so).  Values under about 1e-15 next to an eps that does not cover them: times 2^80, as squares
       // lose bits from 2^-126 on (an error of 2^-150 each, nothing next to 2^-100), and are zero below 2^-150.
-      const float by = above ? 0x1p-80f : 0x1p80f;
-      eps = eps * by * by;
+      const float by = mean < 1.0f ? 0x1p80f : 0x1p-80f;
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[c][i] *= by;
-      sum = squares(sums[1]);
+      mean = squares(sums[1]) * per + eps * by * by;
     }
-    const float inv = rsqrtf(sum * (1.0f / (float)h) + eps);
+    const float inv = rsqrtf(mean);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
       float w[8];
