@@ -369,8 +369,9 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void dense_q8_large_kernel(DenseTa
   work.template store<DT>(t, q_scales, shape, acc);
 }
 
-// The kernel for smaller tiles, bound by the compute units' intake (the fetches alone of 1024 tokens, 4096 -> 4096, take 19 of its
-// 25 us) and by some 100 to 190 clocks around a step's barrier.  While half a step's products run, the other half's or the next step's
+// The kernel for smaller tiles.  The fetches alone of 1024 tokens, 4096 -> 4096, take 19 of its 26 us, and some 100 to 190 clocks go
+// around a step's barrier.  What bounds the fetches is not known: of 517 tokens, 4096 -> 4096 + 2 x 1024 (23 to 25 us), the tiles take in
+// 252 MB, of which three quarters come from the L2s.  While half a step's products run, the other half's or the next step's
 // fragments go from LDS to registers and a later step's pieces from memory to LDS; one barrier a step.
 // grid = tiles (channel tiles of all projections times token tiles)
 template <class DT, int NC, int NT, int WC, int WT, int DEPTH>
@@ -424,9 +425,10 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void dense_q8_small_kernel(DenseTa
 // themselves in chunks of 128 bytes (a cache line of every row).  A wave's chunks go from memory to a ring of DEPTH places in
 // LDS that is its own, eight rows to a load, and from there to the matrix cores: no registers are held by what is in flight,
 // and no wave waits for another until their sums meet at the end.  Wide blocks are for batches whose narrower ones would take a
-// second round of workgroups: 64 tokens, 5120 -> 2 x 13824 (128 channels, 216 workgroups) 35 us, with 32 to 96 channels 40 and more;
-// 8192 -> 28672 47 us (5.1 TB/s) against 53.  One token, 4096 -> 3 x 4096 12.0 us, 64 tokens, 4096 -> 2 x 11008 23 us (weights from
-// memory in all of these): what bounds them is memory and that a compute unit takes in some 40 bytes a nanosecond.
+// second round of workgroups: 64 tokens, 5120 -> 2 x 13824 (128 channels, 216 workgroups) 35 to 37 us, with 32 to 96 channels 40 and more;
+// 8192 -> 28672 47 to 50 us (4.8 to 5.1 TB/s) against 53.  One token, 4096 -> 3 x 4096 12.0 us, 64 tokens, 4096 -> 2 x 11008 23 us
+// (weights from memory in all of these).  Memory bounds the widest; of lines that its L2 does not hold a compute unit takes in some
+// 40 bytes a nanosecond, which bounds one token.  64 tokens, 2 x 11008, reach neither (4.0 TB/s; 28 bytes a nanosecond and unit).
 // grid = (channel blocks of all projections, token blocks)
 template <int CH, int NT, int WAVES, int DEPTH>
 struct DenseFew {
@@ -632,8 +634,10 @@ hipError_t launch_few(const DenseArgs& a, hipStream_t st) {
 
 // The kernels, and what the choice among them goes by: the time of a call is estimated for every one of them and the
 // shortest taken.  The figures below are fits to graph replays of 48 shapes (1 to 4814 tokens, h_in 1024 to 13824, outputs
-// of 1024 to 28672, weights from HBM), with every kernel each: the one chosen took 1.5 % more time than the best of them on
-// average, 10 % at worst.
+// of 1024 to 28672, weights from HBM), with every kernel each, before the few-token kernels' sums began at different places and
+// before there was one of 128 channels: of these shapes the kernel chosen took 1.5 % more time than the best of them on average, 10 % at
+// worst.  That is no bound for others: the estimates hold no fixed time of a launch, and none for units that the one round of a
+// launch leaves idle (300 tokens, 2048 -> 2 x 5504 takes tiles of 128 x 256 on 172 of 256 units and 22.8 us, where 18.8 are possible).
 struct DenseKernel {
   int channels, tokens, threads, lds;
   // Few tokens, 0: a compute unit takes in 40 bytes of w and x a nanosecond, and the workgroups of a launch run in rounds of one to

@@ -12,8 +12,10 @@
 // The maximum is taken of the bit patterns of |v| as unsigned integers, which puts infinities above every number and NaN
 // above those: one comparison against the infinity's pattern tells a row that holds something not finite.
 //
-// Bound by memory: 4814 rows of 8192 with residual, sum and both outputs 67 us (5.3 TB/s; a large copy reaches 5.1), silu
-// of 2900 rows of 13824 54 us (5.2 TB/s), 8190 rows of 4096 into 8 bits 17 us (5.9 TB/s); a single row by the launch (a norm 3.7 us).
+// Bound by memory (replays over more than 1 GB of inputs and outputs, so that no cache serves them; a copy of 1 GiB reaches 5.1 TB/s):
+// 4814 rows of 8192 with residual, sum and both outputs 65 us (5.5 TB/s), silu of 2900 rows of 13824 53 us (5.3), 8190 rows of 4096
+// into 8 bits 21 us (4.8; 16380 rows 37 us, 5.5).  A single row by the launch (a norm 3.6 us), some hundred rows, all of them resident
+// at once, by one chain of launch, loads, reductions and stores (577 rows of 5128 7.5 us).
 #include "device_common.h"
 #include "q8.h"
 
