@@ -167,7 +167,10 @@ typedef enum {
   SGMV_KERNEL_DENSE_FEW = 9,        /* sgmv_dense_q8: few tokens, a workgroup's waves      */
                                     /* divide h_in                                         */
   SGMV_KERNEL_DENSE_SMALL = 10,     /* ... tiles of up to 128 x 128                        */
-  SGMV_KERNEL_DENSE_LARGE = 11      /* ... tiles of up to 256 x 256                        */
+  SGMV_KERNEL_DENSE_LARGE = 11,     /* ... tiles of up to 256 x 256                        */
+  SGMV_KERNEL_ATTENTION_FEW = 12,   /* sgmv_attention_q4: sixteen columns (rows x heads of */
+                                    /* a group), a workgroup's waves divide the positions  */
+  SGMV_KERNEL_ATTENTION_MANY = 13   /* ... its waves divide more columns                   */
 } sgmv_kernel;
 
 /* What a call would launch: plain data filled by sgmv_plan_add_lora. */
@@ -438,6 +441,151 @@ int sgmv_dense_q8(int32_t dtype, int32_t n_proj, void* const* ys, const int8_t* 
  * launches of one kernel).  Returns the status that the call's sizes alone give. */
 int sgmv_plan_dense_q8(int32_t dtype, int32_t n_proj, int32_t n_tokens, int32_t h_in, const int32_t* h_outs,
                        const void* workspace, size_t workspace_bytes, sgmv_plan* plan);
+
+/* ---------------------------------------------------------------------------------------------
+ * Attention over a paged cache held in 4 bits.
+ *
+ * What stands between the q / k / v projections (with their add-ons) and the o projection: a cache
+ * of keys and values in pages, as the paper's separable KvCache layout has it ([pages][layers][..]: requests
+ * join, leave and grow on their own), its values in 4-bit integers with a scale and a minimum per position and head.
+ *
+ *   sgmv_kv_assign     once a step: pages, block tables, slots and positions from the requests' lengths, on the device
+ *   sgmv_kv_append_q4  rotary positions of q and k, then k and v in 4 bits into the cache
+ *   sgmv_attention_q4  attention of every row over its request's pages: prompts, single tokens, both in one call
+ *   sgmv_kv_read_q4    rows of the cache back in 16 bits
+ *
+ * Conventions beyond the general ones above:
+ *   - A row x of head_dim 16-bit values is held as m = min x, s = (max x - m) / 15 and codes c = (x - m) / s, between
+ *     0 and 15, and stands for c * s + m.  s is rounded to the 16-bit type (m needs no rounding; a zero is +0), c to the nearest, ties to
+ *     even; c is 0 where s is 0.  All of it is fp32 (the quotients correctly rounded).  A row in which a value is not finite,
+ *     or max x - m is not, has scale NaN and codes 0: whatever reads it is NaN.
+ *   - Layout: pages [n_pages][num_layers][n_kv_heads][page_size / 16] tiles of 16 positions; a tile is
+ *     8 * head_dim bytes of k's codes (value j of position p: nibble j % 2, low first, of byte p * head_dim / 2 + j / 2), as
+ *     many of v's (byte (p / 4) * 2 head_dim + (j / 8) * 16 + (p % 4) * 4 + (j % 8) / 2), then s and m of k as a pair of 16-bit
+ *     floats for every position, and those of v.
+ *   - Arrays of int32 lie on the device; their contents are not checked on the host.  The kernels take what leads out of a
+ *     buffer as absent: a slot or position out of range is not written, a block table's entry outside
+ *     [0, n_pages) hides the positions of its page, lengths are cut to [0, table_width * page_size] and row ranges to the batch.
+ *   - The descriptors are HOST memory, read during the call only.  16-bit rows are 16-byte aligned, their strides multiples
+ *     of 8 values and at least a row (the heads of a row lie side by side, head_dim values each); pages 16-byte aligned,
+ *     int32, lse and the rotary table 4-byte aligned (else SGMV_ERR_ALIGN, strides SGMV_ERR_SHAPE).
+ *   - Buffers that a call writes must not overlap one another or what it reads, except where said: SGMV_ERR_SHAPE.
+ *     n_reqs == 0 or n_tokens == 0 returns SGMV_OK and enqueues nothing (sgmv_kv_assign runs with n_tokens == 0 too).
+ *   - Calls are asynchronous on `stream`, which belongs to the current device, like the buffers. */
+
+/* The cache: head_dim 64 or 128; page_size 16, 32, 64, 128 or 256; page_size * n_pages below 2^31. */
+typedef struct sgmv_kv_cache {
+  int32_t dtype;             /* sgmv_dtype of q, k, v, out and of the scales and minima     */
+  int32_t head_dim;
+  int32_t n_kv_heads;
+  int32_t num_layers;
+  int32_t page_size;         /* positions of a page                                         */
+  int32_t n_pages;
+  size_t  page_stride;       /* bytes from page to page, a multiple of 16;                  */
+                             /* 0 = sgmv_kv_page_bytes(), pages side by side                */
+  void*   pages;             /* not looked at by sgmv_kv_assign                             */
+} sgmv_kv_cache;
+
+/* The requests and token rows of a step.  sgmv_kv_assign writes the arrays, the other calls read them; a
+ * program that keeps its own tables fills them itself. */
+typedef struct sgmv_kv_batch {
+  int32_t  n_reqs;
+  int32_t  n_tokens;         /* rows of q, k, v and out                                     */
+  int32_t  table_width;      /* pages that a request can have                               */
+  int32_t  max_q_len;        /* most rows of a request and ...                              */
+  int32_t  max_kv_len;       /* ... most positions, hints for launch shapes: 0 = unknown;   */
+                             /* a wrong hint costs speed, never correctness                 */
+  int32_t  reserved;
+  int32_t* q_starts;         /* [n_reqs + 1] row at which each request starts; rows behind  */
+                             /* the last one belong to nobody and are left as they were     */
+  int32_t* kv_lens;          /* [n_reqs] positions of each request, its rows of this step   */
+                             /* (the last ones) among them                                  */
+  int32_t* tables;           /* [n_reqs][table_width] page of positions i * page_size ...   */
+  int32_t* slots;            /* [n_tokens] page * page_size + position in it, or -1         */
+  int32_t* positions;        /* [n_tokens] position of the row in its request, or -1        */
+} sgmv_kv_batch;
+
+/* Rotary positions: the first `dim` values of a head, in pairs (i, i + dim / 2), or (2 i, 2 i + 1) with `adjacent`:
+ *   a' = a * cos - b * sin,  b' = b * cos + a * sin      every product and sum rounded to fp32, then to the 16-bit type
+ * table fp32 [rows][dim], row = position: dim / 2 cosines, then dim / 2 sines; dim a multiple of 16, at most head_dim. */
+typedef struct sgmv_rope {
+  const float* table;
+  int32_t rows;
+  int32_t dim;
+  int32_t adjacent;
+  int32_t reserved;
+} sgmv_rope;
+
+/* Bytes of a page (all layers and heads); 0 where the descriptor is not supported.  Host-only. */
+size_t sgmv_kv_page_bytes(const sgmv_kv_cache* c);
+
+/* Pages for a step, from the requests' lengths alone, so that a captured step needs nothing from the host.
+ *   new_lens    [n_reqs] tokens that each request brings; -1: it is over and its pages go back
+ *   old_lens    [n_reqs] positions it has so far; may be b->kv_lens (in place)
+ *   free_pages  [n_pages] stack of free pages, bottom first;  free_count [1] how many it holds
+ *   free_count_out [1]; may be free_count (in place)
+ *   status      [2] what was wrong with this call (SGMV_KV_*, 0: nothing), and with all calls so far (or-ed to what is there)
+ * Pages of requests that are over are pushed in the order of the requests and of their tables; then every request whose
+ * positions pass the end of its last page pops what it needs, in the same order.  Writes b->kv_lens (old + new, 0 where a
+ * request is over), the new entries of b->tables, b->q_starts (prefix sums of the rows), and every entry of b->slots and b->positions
+ * (-1 behind the last row).  All or nothing: where something is wrong, lengths, tables and stack stay as they were (the
+ * *_out ones become copies), q_starts is 0, and slots and positions are -1, so that the step's other calls do nothing.
+ * Same inputs, same pages.  A page belongs to one request here: tables that share pages are the program's own to keep.  One launch,
+ * two where there are many rows. */
+#define SGMV_KV_NO_PAGES 1   /* the stack holds too few pages                                */
+#define SGMV_KV_TABLE 2      /* a request would have more than table_width pages             */
+#define SGMV_KV_ROWS 4       /* the requests bring more than n_tokens rows                   */
+#define SGMV_KV_LENGTHS 8    /* a length or the count of free pages is out of range          */
+#define SGMV_KV_PAGE 16      /* a row stands on a page that is not of the cache (its slot is */
+                             /* -1; the only fault that does not refuse the step)            */
+int sgmv_kv_assign(const sgmv_kv_cache* c, const sgmv_kv_batch* b, const int32_t* new_lens, const int32_t* old_lens,
+                   int32_t* free_pages, const int32_t* free_count, int32_t* free_count_out, int32_t* status, void* stream);
+
+/* Rotates q and k by the rows' positions and writes k and v, in 4 bits, into the rows' slots.
+ *   q_out, q    16-bit [n_tokens][n_heads][head_dim], row strides q_out_stride and q_stride (in values); q_out may be q; both
+ *               NULL: k alone
+ *   k, v        16-bit [n_tokens][n_kv_heads][head_dim], row stride kv_stride; k itself is left as it is
+ *   rope        NULL: nothing is rotated, and q and q_out are NULL
+ * A row whose position lies outside the rotary table (with `rope`) is skipped altogether, one whose slot lies outside the cache is
+ * not appended (its q is rotated).  Slots of a call differ from one another; of two rows with one slot either one's values, or some
+ * of each, are kept.  b->q_starts, kv_lens and tables are not looked at, nor, without `rope`, positions. */
+int sgmv_kv_append_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t layer_idx, void* q_out, const void* q, const void* k,
+                      const void* v, int32_t n_heads, int64_t q_out_stride, int64_t q_stride, int64_t kv_stride, const sgmv_rope* rope,
+                      void* stream);
+
+/* Rows of the cache in 16 bits, c * s + m rounded once: k and v (either may be NULL), 16-bit [n_rows][n_kv_heads][head_dim] with
+ * row stride kv_stride.  Rows whose slot lies outside the cache are left as they were. */
+int sgmv_kv_read_q4(const sgmv_kv_cache* c, int32_t layer_idx, void* k, void* v, int64_t kv_stride, const int32_t* slots, int32_t n_rows,
+                    void* stream);
+
+/* Attention:
+ *   out[t][h] = sum_p w_p v[p],   w = softmax over the visible p of scale * q[t][h] . k[p],   k and v of head h / (n_heads / n_kv_heads)
+ * Row j of a request with n rows stands at position kv_len - n + j; it sees the positions of its request up to its own (causal; all
+ * of them without), and with a window only those after its own position - window.
+ *   out         16-bit [n_tokens][n_heads][head_dim], row stride out_stride
+ *   lse         fp32 [n_tokens][n_heads] or NULL: natural logarithm of the softmax's sum (to join parts of an attention)
+ *   q           16-bit, row stride q_stride; n_heads a multiple of n_kv_heads
+ *   scale       positive and finite (else SGMV_ERR_UNSUPPORTED)
+ *   window      0: none
+ *   workspace   device scratch, 256-byte aligned, or NULL with 0 bytes: few rows over long contexts are divided over more workgroups where
+ *               their partial sums fit in it (sgmv_attention_workspace_bytes() is enough for all that gain).  It needs no
+ *               preparation and keeps nothing between calls; calls that share it must be ordered.
+ * A row that sees nothing is zeros, its lse -inf.  Sums, maxima and the softmax are fp32; the codes are exact in the matrix cores, q
+ * keeps all its bits next to its row's largest value, and the weights w * s enter as one 16-bit part with 11 bits for bfloat16, two for
+ * binary16.  Rows of q that hold a NaN, an infinity or a value of 2^100 and more are NaN (where they see anything), as is what sees a
+ * position that holds one; positions that a row does not see do not matter, whatever they hold.  The order of the sums depends on the
+ * hints and the workspace, not on the run: same call, same bits.  n_tokens * n_heads below 2^31, else SGMV_ERR_UNSUPPORTED. */
+int sgmv_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t layer_idx, void* out, float* lse, const void* q,
+                      int32_t n_heads, int64_t out_stride, int64_t q_stride, float scale, int32_t causal, int32_t window, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* Workspace that sgmv_attention_q4 would like for such a batch (its hints included); 0 where none helps.  Host-only. */
+size_t sgmv_attention_workspace_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads);
+
+/* Host-only, pure: what sgmv_attention_q4 would launch (`slices` = parts of a request's positions; with more than one a second launch
+ * joins them).  Returns the status that the call's sizes alone give. */
+int sgmv_plan_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, const void* workspace, size_t workspace_bytes,
+                           sgmv_plan* plan);
 
 /* Measurement aid, not part of the operator: enqueue one plain kernel of known traffic on
  * `stream`, for the benchmark's attainable-bandwidth figure and for scaling a profiler's HBM

@@ -15,6 +15,9 @@ _BINDING_NAMES = (
     "STATIC_SCRATCH_BYTES", "STATIC_MAX_WORKSPACE_BYTES",
     "sgmv_rms_norm_q8", "sgmv_silu_mul_q8", "sgmv_quantize_q8", "sgmv_dense_q8", "sgmv_plan_dense_q8", "DENSE_WORKSPACE_BYTES",
     "KERNEL_DENSE_FEW", "KERNEL_DENSE_SMALL", "KERNEL_DENSE_LARGE",
+    "SgmvKvCache", "SgmvKvBatch", "SgmvRope", "make_kv_cache", "make_kv_batch", "make_rope", "sgmv_kv_page_bytes", "sgmv_kv_assign",
+    "sgmv_kv_append_q4", "sgmv_kv_read_q4", "sgmv_attention_q4", "sgmv_attention_workspace_bytes", "sgmv_plan_attention_q4",
+    "KV_NO_PAGES", "KV_TABLE", "KV_ROWS", "KV_LENGTHS", "KV_PAGE", "KERNEL_ATTENTION_FEW", "KERNEL_ATTENTION_MANY",
 )
 __all__ = list(_BINDING_NAMES)
 

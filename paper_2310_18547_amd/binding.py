@@ -62,12 +62,55 @@ class SgmvPlan(ctypes.Structure):
     ]
 
 
+class SgmvKvCache(ctypes.Structure):
+    """Mirror of ``struct sgmv_kv_cache``."""
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("num_layers", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("page_stride", ctypes.c_size_t),
+        ("pages", ctypes.c_void_p),
+    ]
+
+
+class SgmvKvBatch(ctypes.Structure):
+    """Mirror of ``struct sgmv_kv_batch``."""
+    _fields_ = [
+        ("n_reqs", ctypes.c_int32),
+        ("n_tokens", ctypes.c_int32),
+        ("table_width", ctypes.c_int32),
+        ("max_q_len", ctypes.c_int32),
+        ("max_kv_len", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("q_starts", ctypes.c_void_p),
+        ("kv_lens", ctypes.c_void_p),
+        ("tables", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
+    ]
+
+
+class SgmvRope(ctypes.Structure):
+    """Mirror of ``struct sgmv_rope``."""
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("rows", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("adjacent", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 KERNEL_NONE, KERNEL_FUSED, KERNEL_TILE, KERNEL_MULTI_SIDE, KERNEL_MULTI_PIPELINED, KERNEL_VECTOR, \
-    KERNEL_MATRIX, KERNEL_SEQUENCE, KERNEL_WHOLE, KERNEL_DENSE_FEW, KERNEL_DENSE_SMALL, KERNEL_DENSE_LARGE = range(12)
+    KERNEL_MATRIX, KERNEL_SEQUENCE, KERNEL_WHOLE, KERNEL_DENSE_FEW, KERNEL_DENSE_SMALL, KERNEL_DENSE_LARGE, \
+    KERNEL_ATTENTION_FEW, KERNEL_ATTENTION_MANY = range(14)
 KERNEL_NAMES = {KERNEL_NONE: "none", KERNEL_FUSED: "fused", KERNEL_TILE: "tile",
                 KERNEL_MULTI_SIDE: "multi_side", KERNEL_MULTI_PIPELINED: "multi_pipelined",
                 KERNEL_VECTOR: "vector", KERNEL_MATRIX: "matrix", KERNEL_WHOLE: "whole", KERNEL_DENSE_FEW: "dense_few",
-                KERNEL_DENSE_SMALL: "dense_small", KERNEL_DENSE_LARGE: "dense_large"}
+                KERNEL_DENSE_SMALL: "dense_small", KERNEL_DENSE_LARGE: "dense_large", KERNEL_ATTENTION_FEW: "attention_few", KERNEL_ATTENTION_MANY: "attention_many"}
 
 
 def _load():
@@ -118,6 +161,23 @@ def _load():
     L.sgmv_plan_dense_q8.argtypes = [c.c_int32, c.c_int32, c.c_int32, c.c_int32, c.c_void_p, c.c_void_p, c.c_size_t,
                                      c.POINTER(SgmvPlan)]
     L.sgmv_plan_dense_q8.restype = c.c_int
+    C, KB, R = c.POINTER(SgmvKvCache), c.POINTER(SgmvKvBatch), c.POINTER(SgmvRope)
+    L.sgmv_kv_page_bytes.argtypes = [C]
+    L.sgmv_kv_page_bytes.restype = c.c_size_t
+    L.sgmv_kv_assign.argtypes = [C, KB] + [c.c_void_p] * 7
+    L.sgmv_kv_assign.restype = c.c_int
+    L.sgmv_kv_append_q4.argtypes = [C, KB, c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int32, c.c_int64, c.c_int64,
+                                    c.c_int64, R, c.c_void_p]
+    L.sgmv_kv_append_q4.restype = c.c_int
+    L.sgmv_kv_read_q4.argtypes = [C, c.c_int32, c.c_void_p, c.c_void_p, c.c_int64, c.c_void_p, c.c_int32, c.c_void_p]
+    L.sgmv_kv_read_q4.restype = c.c_int
+    L.sgmv_attention_q4.argtypes = [C, KB, c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int32, c.c_int64, c.c_int64, c.c_float,
+                                    c.c_int32, c.c_int32, c.c_void_p, c.c_size_t, c.c_void_p]
+    L.sgmv_attention_q4.restype = c.c_int
+    L.sgmv_attention_workspace_bytes.argtypes = [C, KB, c.c_int32]
+    L.sgmv_attention_workspace_bytes.restype = c.c_size_t
+    L.sgmv_plan_attention_q4.argtypes = [C, KB, c.c_int32, c.c_void_p, c.c_size_t, c.POINTER(SgmvPlan)]
+    L.sgmv_plan_attention_q4.restype = c.c_int
     L.sgmv_probe.argtypes = [c.c_int, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
     L.sgmv_probe.restype = c.c_int
     L.sgmv_plan_add_lora.argtypes = [P, c.c_int32, c.c_int32, c.POINTER(SgmvPlan)]
@@ -158,6 +218,31 @@ def make_problem(dtype: int, h_in: int, h_out: int, r: int, num_layers: int, n_t
                        expand_threads, workspace_ready, spin_limit, _addr(workspace), workspace_bytes)
 
 
+def make_kv_cache(dtype: int, head_dim: int, n_kv_heads: int, num_layers: int, page_size: int, n_pages: int, pages=None,
+                  page_stride: int = 0) -> SgmvKvCache:
+    return SgmvKvCache(dtype, head_dim, n_kv_heads, num_layers, page_size, n_pages, page_stride, _addr(pages))
+
+
+def make_kv_batch(n_reqs: int, n_tokens: int, table_width: int, q_starts, kv_lens, tables, slots=None, positions=None,
+                  max_q_len: int = 0, max_kv_len: int = 0) -> SgmvKvBatch:
+    """The descriptor holds addresses alone: keep the arrays."""
+    return SgmvKvBatch(n_reqs, n_tokens, table_width, max_q_len, max_kv_len, 0, _addr(q_starts), _addr(kv_lens), _addr(tables),
+                       _addr(slots), _addr(positions))
+
+
+def make_rope(table, rows: int, dim: int, adjacent: int = 0) -> SgmvRope:
+    """``table``: fp32 ``[rows][dim]``, cosines then sines (kept by the caller)."""
+    return SgmvRope(_addr(table), rows, dim, adjacent, 0)
+
+
+def sgmv_kv_page_bytes(cache: SgmvKvCache) -> int:
+    return int(lib.sgmv_kv_page_bytes(ctypes.byref(cache)))
+
+
+def sgmv_attention_workspace_bytes(cache: SgmvKvCache, batch: SgmvKvBatch, n_heads: int) -> int:
+    return int(lib.sgmv_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads))
+
+
 def sgmv_status_string(status: int) -> str:
     return lib.sgmv_status_string(int(status)).decode()
 
@@ -188,6 +273,8 @@ def sgmv_validate_segments(host_seg_starts, n_segs: int, n_tokens: int) -> int:
 STATIC_SCRATCH_BYTES = 9 << 20
 STATIC_MAX_WORKSPACE_BYTES = 8 << 20
 DENSE_WORKSPACE_BYTES = 16 << 20
+# what sgmv_kv_assign's status says, or-ed together
+KV_NO_PAGES, KV_TABLE, KV_ROWS, KV_LENGTHS, KV_PAGE = 1, 2, 4, 8, 16
 
 
 class ArgumentError(ctypes.ArgumentError, TypeError):
@@ -266,6 +353,31 @@ class _General:
                      arr(*[_addr(a) for a in ws]), arr(*[_addr(a) for a in w_scales]), n_tokens, h_in,
                      (ctypes.c_int32 * n)(*h_outs), _addr(workspace), workspace_bytes, _stream(stream))
 
+    @staticmethod
+    def sgmv_kv_assign(cache: SgmvKvCache, batch: SgmvKvBatch, new_lens, old_lens, free_pages, free_count, free_count_out, status,
+                       stream=None, check: bool = True) -> int:
+        return _call("sgmv_kv_assign", check, ctypes.byref(cache), ctypes.byref(batch), _addr(new_lens), _addr(old_lens),
+                     _addr(free_pages), _addr(free_count), _addr(free_count_out), _addr(status), _stream(stream))
+
+    @staticmethod
+    def sgmv_kv_append_q4(cache: SgmvKvCache, batch: SgmvKvBatch, layer_idx: int, q_out, q, k, v, n_heads: int, q_out_stride: int,
+                          q_stride: int, kv_stride: int, rope: Optional[SgmvRope] = None, stream=None, check: bool = True) -> int:
+        return _call("sgmv_kv_append_q4", check, ctypes.byref(cache), ctypes.byref(batch), layer_idx, _addr(q_out), _addr(q), _addr(k),
+                     _addr(v), n_heads, q_out_stride, q_stride, kv_stride, None if rope is None else ctypes.byref(rope), _stream(stream))
+
+    @staticmethod
+    def sgmv_kv_read_q4(cache: SgmvKvCache, layer_idx: int, k, v, kv_stride: int, slots, n_rows: int, stream=None,
+                        check: bool = True) -> int:
+        return _call("sgmv_kv_read_q4", check, ctypes.byref(cache), layer_idx, _addr(k), _addr(v), kv_stride, _addr(slots), n_rows,
+                     _stream(stream))
+
+    @staticmethod
+    def sgmv_attention_q4(cache: SgmvKvCache, batch: SgmvKvBatch, layer_idx: int, out, lse, q, n_heads: int, out_stride: int,
+                          q_stride: int, scale: float, causal: int = 1, window: int = 0, workspace=None, workspace_bytes: int = 0,
+                          stream=None, check: bool = True) -> int:
+        return _call("sgmv_attention_q4", check, ctypes.byref(cache), ctypes.byref(batch), layer_idx, _addr(out), _addr(lse), _addr(q),
+                     n_heads, out_stride, q_stride, scale, causal, window, _addr(workspace), workspace_bytes, _stream(stream))
+
 
 def _calls():
     """The per-layer calls, their usual arguments marshalled in C (csrc/call_module.c)."""
@@ -275,15 +387,31 @@ def _calls():
         raise ImportError(f"{_HERE} holds no _sgmv_call module for this interpreter: build it with "
                           "`python -m paper_2310_18547_amd.build`") from e
     names = ("sgmv_shrink", "sgmv_expand", "sgmv_add_lora", "sgmv_add_lora_static", "sgmv_add_lora_multi",
-             "sgmv_rms_norm_q8", "sgmv_silu_mul_q8", "sgmv_quantize_q8", "sgmv_dense_q8")
-    size = module.bind(SgmvProblem, SgmvError, tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names),
+             "sgmv_rms_norm_q8", "sgmv_silu_mul_q8", "sgmv_quantize_q8", "sgmv_dense_q8", "sgmv_kv_assign", "sgmv_kv_append_q4",
+             "sgmv_kv_read_q4", "sgmv_attention_q4")
+    structs = (SgmvProblem, SgmvKvCache, SgmvKvBatch, SgmvRope)
+    sizes = module.bind(structs, SgmvError, tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names),
                        tuple(getattr(_General, n) for n in names))
-    assert size == ctypes.sizeof(SgmvProblem)
+    assert sizes == tuple(ctypes.sizeof(t) for t in structs)
     return [getattr(module, n) for n in names]
 
 
 (sgmv_shrink, sgmv_expand, sgmv_add_lora, sgmv_add_lora_static, sgmv_add_lora_multi,
- sgmv_rms_norm_q8, sgmv_silu_mul_q8, sgmv_quantize_q8, sgmv_dense_q8) = _calls()
+ sgmv_rms_norm_q8, sgmv_silu_mul_q8, sgmv_quantize_q8, sgmv_dense_q8, sgmv_kv_assign, sgmv_kv_append_q4, sgmv_kv_read_q4,
+ sgmv_attention_q4) = _calls()
+
+
+def sgmv_plan_attention_q4(cache: SgmvKvCache, batch: SgmvKvBatch, n_heads: int, workspace=None, workspace_bytes: int = 0,
+                           check: bool = True):
+    """Host-only: the ``SgmvPlan`` of a ``sgmv_attention_q4`` call (``check=False``: ``(status, plan)``)."""
+    plan = SgmvPlan()
+    rc = lib.sgmv_plan_attention_q4(ctypes.byref(cache), ctypes.byref(batch), n_heads, _addr(workspace), workspace_bytes,
+                                    ctypes.byref(plan))
+    if not check:
+        return rc, plan
+    if rc != 0:
+        raise SgmvError(rc, "sgmv_plan_attention_q4")
+    return plan
 
 
 def sgmv_plan_expand(p: SgmvProblem, n_segs: int, check: bool = True):

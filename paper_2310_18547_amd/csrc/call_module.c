@@ -35,6 +35,14 @@ typedef int (*quantize_fn)(int32_t, int8_t*, float*, const void*, int32_t, int32
 typedef int (*dense_fn)(int32_t, int32_t, void* const*, const int8_t*, const float*, const int8_t* const*, const float* const*,
                         int32_t, int32_t, const int32_t*, void*, size_t, void*);
 
+typedef int (*kv_assign_fn)(const sgmv_kv_cache*, const sgmv_kv_batch*, const int32_t*, const int32_t*, int32_t*, const int32_t*, int32_t*,
+                            int32_t*, void*);
+typedef int (*kv_append_fn)(const sgmv_kv_cache*, const sgmv_kv_batch*, int32_t, void*, const void*, const void*, const void*, int32_t, int64_t,
+                            int64_t, int64_t, const sgmv_rope*, void*);
+typedef int (*kv_read_fn)(const sgmv_kv_cache*, int32_t, void*, void*, int64_t, const int32_t*, int32_t, void*);
+typedef int (*attention_fn)(const sgmv_kv_cache*, const sgmv_kv_batch*, int32_t, void*, float*, const void*, int32_t, int64_t, int64_t, float,
+                            int32_t, int32_t, void*, size_t, void*);
+
 static shrink_fn fn_shrink;
 static expand_fn fn_expand;
 static add_lora_fn fn_add_lora;
@@ -44,9 +52,15 @@ static rms_norm_fn fn_rms_norm;
 static silu_mul_fn fn_silu_mul;
 static quantize_fn fn_quantize;
 static dense_fn fn_dense;
-static PyObject* problem_type;  // binding.SgmvProblem
+static kv_assign_fn fn_kv_assign;
+static kv_append_fn fn_kv_append;
+static kv_read_fn fn_kv_read;
+static attention_fn fn_attention;
+enum { PROBLEM, KV_CACHE, KV_BATCH, ROPE, STRUCTS };
+static PyObject* struct_types[STRUCTS];  // binding.SgmvProblem, SgmvKvCache, SgmvKvBatch, SgmvRope
 static PyObject* error_type;    // binding.SgmvError
-enum { SHRINK, EXPAND, ADD_LORA, ADD_LORA_STATIC, ADD_LORA_MULTI, RMS_NORM, SILU_MUL, QUANTIZE, DENSE, CALLS };
+enum { SHRINK, EXPAND, ADD_LORA, ADD_LORA_STATIC, ADD_LORA_MULTI, RMS_NORM, SILU_MUL, QUANTIZE, DENSE,
+       KV_ASSIGN, KV_APPEND, KV_READ, ATTENTION, CALLS };
 static PyObject* general[CALLS];  // the functions in Python, in the order of bind()'s addresses
 static PyObject *str_data_ptr, *str_cuda_stream;
 
@@ -110,13 +124,14 @@ static int float_of(PyObject* o, float* out) {
   return DONE;
 }
 
-// The caller's struct sgmv_problem; PyBuffer_Release when done.
-static int problem_of(PyObject* o, Py_buffer* view) {
-  const int is = PyObject_IsInstance(o, problem_type);
+// The caller's struct of that type; PyBuffer_Release when done.
+static int struct_of(PyObject* o, int which, Py_buffer* view) {
+  const int is = PyObject_IsInstance(o, struct_types[which]);
   if (is < 0) return -1;
   if (!is) return UNUSUAL;
   return PyObject_GetBuffer(o, view, PyBUF_SIMPLE);
 }
+static int problem_of(PyObject* o, Py_buffer* view) { return struct_of(o, PROBLEM, view); }
 
 // Positional and keyword arguments into `got` by name; the first `required` must be there.
 static int sort_arguments(const char* const* names, int n, int required, PyObject* const* args, Py_ssize_t nargs,
@@ -411,13 +426,148 @@ static PyObject* call_dense(PyObject* self, PyObject* const* args, Py_ssize_t na
   return finish(rc, g[12], "sgmv_dense_q8");
 }
 
-// bind(problem type, error type, then of the calls, in the order of the enumeration above, the
+static int int64_of(PyObject* o, int64_t* out) {
+  if (!PyLong_Check(o)) return UNUSUAL;
+  const long long v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) return unusual();
+  *out = v;
+  return DONE;
+}
+
+// Up to three structs of a call at once: all of them, or none is held.  An absent last one (None or left out) has no address.
+typedef struct {
+  Py_buffer views[3];
+  int n;
+} Structs;
+static int structs_of(Structs* s, PyObject* const* objects, const int* types, int n) {
+  s->n = 0;
+  for (int i = 0; i < n; ++i) {
+    s->views[i].buf = NULL;
+    s->views[i].obj = NULL;
+    if (i == 2 && (objects[i] == NULL || objects[i] == Py_None)) continue;
+    const int rc = struct_of(objects[i], types[i], &s->views[i]);
+    if (rc != DONE) {
+      while (s->n > 0) PyBuffer_Release(&s->views[--s->n]);
+      return rc;
+    }
+    s->n = i + 1;
+  }
+  return DONE;
+}
+static void structs_done(Structs* s) {
+  while (s->n > 0) PyBuffer_Release(&s->views[--s->n]);
+}
+static const int kv_types[] = {KV_CACHE, KV_BATCH, ROPE};
+
+static PyObject* call_kv_assign(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"cache", "batch", "new_lens", "old_lens", "free_pages", "free_count", "free_count_out", "status",
+                                      "stream", "check"};
+  PyObject* g[10];
+  void *a[6], *stream;  // new_lens .. status
+  Structs s;
+  int rc = sort_arguments(names, 10, 8, args, nargs, kwnames, g);
+  for (int i = 0; i < 6; ++i) FIRST(address_of(g[2 + i], &a[i]));
+  FIRST(stream_of(g[8], &stream));
+  FIRST(structs_of(&s, g, kv_types, 2));
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[KV_ASSIGN], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_kv_assign(s.views[0].buf, s.views[1].buf, a[0], a[1], a[2], a[3], a[4], a[5], stream);
+  Py_END_ALLOW_THREADS
+  structs_done(&s);
+  return finish(rc, g[9], "sgmv_kv_assign");
+}
+
+static PyObject* call_kv_append(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"cache", "batch", "layer_idx", "q_out", "q", "k", "v", "n_heads", "q_out_stride", "q_stride",
+                                      "kv_stride", "rope", "stream", "check"};
+  PyObject* g[14];
+  void *a[4], *stream;  // q_out .. v
+  int32_t layer, n_heads;
+  int64_t strides[3];
+  Structs s;
+  int rc = sort_arguments(names, 14, 11, args, nargs, kwnames, g);
+  FIRST(int32_of(g[2], &layer));
+  for (int i = 0; i < 4; ++i) FIRST(address_of(g[3 + i], &a[i]));
+  FIRST(int32_of(g[7], &n_heads));
+  for (int i = 0; i < 3; ++i) FIRST(int64_of(g[8 + i], &strides[i]));
+  FIRST(stream_of(g[12], &stream));
+  if (rc == DONE) {
+    PyObject* const objects[] = {g[0], g[1], g[11]};
+    rc = structs_of(&s, objects, kv_types, 3);
+  }
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[KV_APPEND], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_kv_append(s.views[0].buf, s.views[1].buf, layer, a[0], a[1], a[2], a[3], n_heads, strides[0], strides[1], strides[2],
+                    s.views[2].buf, stream);
+  Py_END_ALLOW_THREADS
+  structs_done(&s);
+  return finish(rc, g[13], "sgmv_kv_append_q4");
+}
+
+static PyObject* call_kv_read(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"cache", "layer_idx", "k", "v", "kv_stride", "slots", "n_rows", "stream", "check"};
+  PyObject* g[9];
+  void *k, *v, *slots, *stream;
+  int32_t layer, n_rows;
+  int64_t stride;
+  Structs s;
+  int rc = sort_arguments(names, 9, 7, args, nargs, kwnames, g);
+  FIRST(int32_of(g[1], &layer));
+  FIRST(address_of(g[2], &k));
+  FIRST(address_of(g[3], &v));
+  FIRST(int64_of(g[4], &stride));
+  FIRST(address_of(g[5], &slots));
+  FIRST(int32_of(g[6], &n_rows));
+  FIRST(stream_of(g[7], &stream));
+  FIRST(structs_of(&s, g, kv_types, 1));
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[KV_READ], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_kv_read(s.views[0].buf, layer, k, v, stride, slots, n_rows, stream);
+  Py_END_ALLOW_THREADS
+  structs_done(&s);
+  return finish(rc, g[8], "sgmv_kv_read_q4");
+}
+
+static PyObject* call_attention(PyObject* self, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const names[] = {"cache", "batch", "layer_idx", "out", "lse", "q", "n_heads", "out_stride", "q_stride", "scale",
+                                      "causal", "window", "workspace", "workspace_bytes", "stream", "check"};
+  PyObject* g[16];
+  void *out, *lse, *q, *workspace, *stream;
+  int32_t layer, n_heads, causal = 1, window = 0;
+  int64_t strides[2];
+  float scale;
+  size_t bytes;
+  Structs s;
+  int rc = sort_arguments(names, 16, 10, args, nargs, kwnames, g);
+  FIRST(int32_of(g[2], &layer));
+  FIRST(address_of(g[3], &out));
+  FIRST(address_of(g[4], &lse));
+  FIRST(address_of(g[5], &q));
+  FIRST(int32_of(g[6], &n_heads));
+  for (int i = 0; i < 2; ++i) FIRST(int64_of(g[7 + i], &strides[i]));
+  FIRST(float_of(g[9], &scale));
+  if (rc == DONE && g[10] != NULL) rc = int32_of(g[10], &causal);
+  if (rc == DONE && g[11] != NULL) rc = int32_of(g[11], &window);
+  FIRST(address_of(g[12] == NULL ? Py_None : g[12], &workspace));
+  FIRST(size_of(g[13], &bytes));
+  FIRST(stream_of(g[14], &stream));
+  FIRST(structs_of(&s, g, kv_types, 2));
+  if (rc != DONE) return rc < 0 ? NULL : PyObject_Vectorcall(general[ATTENTION], args, nargs, kwnames);
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn_attention(s.views[0].buf, s.views[1].buf, layer, out, lse, q, n_heads, strides[0], strides[1], scale, causal, window, workspace,
+                    bytes, stream);
+  Py_END_ALLOW_THREADS
+  structs_done(&s);
+  return finish(rc, g[15], "sgmv_attention_q4");
+}
+
+// bind(struct types, error type, then of the calls, in the order of the enumeration above, the
 // addresses and the functions in Python)
 static PyObject* call_bind(PyObject* self, PyObject* args) {
-  PyObject *problem, *error, *addresses, *functions;
-  if (!PyArg_ParseTuple(args, "OOO!O!", &problem, &error, &PyTuple_Type, &addresses, &PyTuple_Type, &functions)) return NULL;
-  if (PyTuple_GET_SIZE(addresses) != CALLS || PyTuple_GET_SIZE(functions) != CALLS) {
-    PyErr_SetString(PyExc_ValueError, "an address and a function for every call");
+  PyObject *structs, *error, *addresses, *functions;
+  if (!PyArg_ParseTuple(args, "O!OO!O!", &PyTuple_Type, &structs, &error, &PyTuple_Type, &addresses, &PyTuple_Type, &functions)) return NULL;
+  if (PyTuple_GET_SIZE(structs) != STRUCTS || PyTuple_GET_SIZE(addresses) != CALLS || PyTuple_GET_SIZE(functions) != CALLS) {
+    PyErr_SetString(PyExc_ValueError, "a type for every struct, an address and a function for every call");
     return NULL;
   }
   unsigned long long f[CALLS];
@@ -425,9 +575,12 @@ static PyObject* call_bind(PyObject* self, PyObject* args) {
     f[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i));
     if (f[i] == (unsigned long long)-1 && PyErr_Occurred()) return NULL;
   }
-  Py_INCREF(problem);
+  for (int i = 0; i < STRUCTS; ++i) {
+    PyObject* type = PyTuple_GET_ITEM(structs, i);
+    Py_INCREF(type);
+    Py_XSETREF(struct_types[i], type);
+  }
   Py_INCREF(error);
-  Py_XSETREF(problem_type, problem);
   Py_XSETREF(error_type, error);
   for (int i = 0; i < CALLS; ++i) {
     PyObject* function = PyTuple_GET_ITEM(functions, i);
@@ -443,7 +596,12 @@ static PyObject* call_bind(PyObject* self, PyObject* args) {
   fn_silu_mul = (silu_mul_fn)(uintptr_t)f[SILU_MUL];
   fn_quantize = (quantize_fn)(uintptr_t)f[QUANTIZE];
   fn_dense = (dense_fn)(uintptr_t)f[DENSE];
-  return PyLong_FromSize_t(sizeof(sgmv_problem));
+  fn_kv_assign = (kv_assign_fn)(uintptr_t)f[KV_ASSIGN];
+  fn_kv_append = (kv_append_fn)(uintptr_t)f[KV_APPEND];
+  fn_kv_read = (kv_read_fn)(uintptr_t)f[KV_READ];
+  fn_attention = (attention_fn)(uintptr_t)f[ATTENTION];
+  return Py_BuildValue("nnnn", (Py_ssize_t)sizeof(sgmv_problem), (Py_ssize_t)sizeof(sgmv_kv_cache), (Py_ssize_t)sizeof(sgmv_kv_batch),
+                       (Py_ssize_t)sizeof(sgmv_rope));
 }
 
 #define FAST(name, fn, doc) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL | METH_KEYWORDS, doc}
@@ -468,7 +626,17 @@ static PyMethodDef methods[] = {
     FAST("sgmv_dense_q8", call_dense,
          "sgmv_dense_q8(dtype, ys, q, q_scales, ws, w_scales, n_tokens, h_in, h_outs, workspace=None, workspace_bytes=0, "
          "stream=None, check=True)\n--\n\nys, ws, w_scales, h_outs are sequences of equal length (one entry per projection)."),
-    {"bind", call_bind, METH_VARARGS, "bind(problem_type, error_type, addresses, functions) -> size of the C struct"},
+    FAST("sgmv_kv_assign", call_kv_assign,
+         "sgmv_kv_assign(cache, batch, new_lens, old_lens, free_pages, free_count, free_count_out, status, stream=None, check=True)\n--\n\n"),
+    FAST("sgmv_kv_append_q4", call_kv_append,
+         "sgmv_kv_append_q4(cache, batch, layer_idx, q_out, q, k, v, n_heads, q_out_stride, q_stride, kv_stride, rope=None, stream=None, "
+         "check=True)\n--\n\n"),
+    FAST("sgmv_kv_read_q4", call_kv_read,
+         "sgmv_kv_read_q4(cache, layer_idx, k, v, kv_stride, slots, n_rows, stream=None, check=True)\n--\n\n"),
+    FAST("sgmv_attention_q4", call_attention,
+         "sgmv_attention_q4(cache, batch, layer_idx, out, lse, q, n_heads, out_stride, q_stride, scale, causal=1, window=0, workspace=None, "
+         "workspace_bytes=0, stream=None, check=True)\n--\n\n"),
+    {"bind", call_bind, METH_VARARGS, "bind(struct_types, error_type, addresses, functions) -> sizes of the C structs"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sgmv_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

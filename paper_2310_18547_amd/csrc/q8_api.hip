@@ -5,22 +5,11 @@
 #include "../../include/sgmv.h"
 #include "launch.h"
 #include "q8.h"
+#include "spans.h"
 
 namespace {
 
 using namespace sgmv;
-
-inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-// A device buffer of a call; none at all where `at` is nullptr.
-struct Span {
-  const void* at;
-  size_t bytes;
-};
-inline bool overlap(const Span& a, const Span& b) {
-  const uintptr_t from = reinterpret_cast<uintptr_t>(a.at), to = reinterpret_cast<uintptr_t>(b.at);
-  return a.at != nullptr && b.at != nullptr && (to - from < a.bytes || from - to < b.bytes);
-}
 
 int check_rows(int32_t dtype, int32_t n_tokens, int32_t h) {
   if (dtype != SGMV_F16 && dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
