@@ -61,8 +61,8 @@ struct KvReadArgs {
 };
 hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st);
 
-// Columns of an attention tile: rows x query heads of one cache head's group, row by row.
-constexpr int kFewColumns = 16;
+// Columns of an attention workgroup's tile: rows x query heads of one cache head's group, row by row.
+constexpr int kFewColumns = 16, kSomeColumns = 64, kManyColumns = 128;
 // Positions of one step of a wave.
 constexpr int kStepPositions = 32;
 struct AttentionArgs {
@@ -72,6 +72,7 @@ struct AttentionArgs {
   int n_heads, group, n_reqs, n_tokens, table_width;
   int causal, window;
   float scale;
+  int columns;               // one of the three
   uint16_t* out;
   float* lse;
   const uint16_t* q;
@@ -84,7 +85,7 @@ struct AttentionArgs {
   float* sums;               // slices > 1: [n_tokens][n_heads][slices][head_dim] unnormalised, then ...
   float2* tops;              // ... {maximum in powers of two, sum} of each
 };
-hipError_t launch_attention_few(const AttentionArgs& a, hipStream_t st);
+hipError_t launch_attention(const AttentionArgs& a, hipStream_t st);
 hipError_t launch_attention_join(const AttentionArgs& a, hipStream_t st);
 
 // Tiles of so many columns: a request's may start in the middle of one of the batch's, so each adds one.

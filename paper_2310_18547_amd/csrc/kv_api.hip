@@ -89,19 +89,25 @@ int check_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_he
 }
 
 struct AttentionPlan {
-  int slices, slice_steps;
+  int columns, slices, slice_steps;
   long long workgroups;
 };
 size_t slice_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads) {
   return (size_t)b->n_tokens * (size_t)n_heads * (4 * (size_t)c->head_dim + 8);
+}
+// Columns of a workgroup for requests of so many rows.
+int columns_of(const sgmv_kv_batch* b, int32_t n_kv_heads, long long group, long long rows) {
+  if (rows * group <= kFewColumns) return kFewColumns;
+  return attention_tiles(b->n_tokens, (int)group, b->n_reqs, kManyColumns) * n_kv_heads >= 4LL * compute_units() || rows * group <= 32 ? kManyColumns : kSomeColumns;
 }
 // `room`: bytes of workspace.
 AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, size_t room) {
   const long long group = n_heads / c->n_kv_heads, covered = (long long)b->table_width * c->page_size;
   const long long longest = b->max_kv_len > 0 && b->max_kv_len < covered ? b->max_kv_len : covered;
   const long long rows = b->max_q_len > 0 ? b->max_q_len : (b->n_tokens + b->n_reqs - 1LL) / b->n_reqs;
-  const long long all = attention_tiles(b->n_tokens, (int)group, b->n_reqs, kFewColumns);
-  const long long busiest = b->n_reqs * ((rows * group + kFewColumns - 1) / kFewColumns);
+  const int columns = columns_of(b, c->n_kv_heads, group, rows);
+  const long long all = attention_tiles(b->n_tokens, (int)group, b->n_reqs, columns);
+  const long long busiest = b->n_reqs * ((rows * group + columns - 1) / columns);
   const long long groups = (all < busiest ? all : busiest) * c->n_kv_heads;
   const long long steps = (longest + kStepPositions - 1) / kStepPositions;
   long long slices = ((long long)kGroupsPerUnit * compute_units() + groups - 1) / groups;
@@ -112,7 +118,7 @@ AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int
   if (slices < 2) slices = 1;
   if (slices > 4096) slices = 4096;
   const long long per = (steps + slices - 1) / slices;
-  return {(int)slices, (int)(per > 0 ? per : 1), all * c->n_kv_heads * slices};
+  return {columns, (int)slices, (int)(per > 0 ? per : 1), all * c->n_kv_heads * slices};
 }
 
 }  // namespace
@@ -274,12 +280,13 @@ int sgmv_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t la
   a.q_starts = b->q_starts;
   a.kv_lens = b->kv_lens;
   a.tables = b->tables;
+  a.columns = plan.columns;
   a.slices = plan.slices;
   a.slice_steps = plan.slice_steps;
   a.sums = static_cast<float*>(workspace);
   a.tops = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + (size_t)n * n_heads * plan.slices * 4 * c->head_dim);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t err = launch_attention_few(a, st);
+  hipError_t err = launch_attention(a, st);
   if (err == hipSuccess && plan.slices > 1) err = launch_attention_join(a, st);
   return err == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
 }
@@ -299,7 +306,7 @@ int sgmv_plan_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32
   const int rc = check_attention(c, b, n_heads, workspace, workspace_bytes, &nothing);
   if (rc != SGMV_OK || nothing) return rc;
   const AttentionPlan p = plan_attention(c, b, n_heads, workspace == nullptr ? 0 : workspace_bytes);
-  plan->kernel = SGMV_KERNEL_ATTENTION_FEW;
+  plan->kernel = p.columns == kFewColumns ? SGMV_KERNEL_ATTENTION_FEW : SGMV_KERNEL_ATTENTION_MANY;
   plan->launches = p.slices > 1 ? 2 : 1;
   plan->slices = p.slices;
   plan->workgroups = p.workgroups > INT32_MAX ? INT32_MAX : (int32_t)p.workgroups;

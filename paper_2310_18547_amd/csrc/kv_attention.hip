@@ -4,14 +4,19 @@
 //   with k_p = s c + m (codes c of 4 bits, scale and minimum of the position):
 //   q . k_p = s (sum_j q_j c_j) + m sum_j q_j,       sum_p w_p v_p = sum_p (w_p s_p) c_p + sum_p w_p m_p
 //
-// so the codes go to the matrix cores as they are, and scales and minima touch scores and weights alone.  A code c
-// masked out of its word is the binary16 number c * 2^-24 (or, one nibble higher, 16 c * 2^-24), exactly: the matrix cores take
-// these as they take any other, five instructions make eight operands of a word, and the powers of two go into q and out.
+// so the codes go to the matrix cores as they are, and scales and minima touch scores and weights alone.  A code c in bits 4 to 7 of
+// a half word, everything else masked out, is the binary16 number 16 c * 2^-24, exactly: seven instructions make eight operands of
+// a word.  (Those cores cut products with numbers below 2^-14 off at a fixed place: of codes in bits 0 to 3 the sum of 32 products is
+// off by 2^-21.8 of their size on average, always downwards, of bits 4 to 7 by a sixteenth of that.)
+//
+// Sums of many positive w s c that nearly cancel against the minima would lose what is left of them: v's odd positions are taken from
+// their largest value down, v = (m + 15 s) - s (15 - c), which costs an inversion of their words, so that terms of both signs add up.
 //
 // Columns are rows x query heads of one cache head's group; sixteen of them make a tile.  S^T = K q^T has positions as rows, so a lane
 // receives four positions of its column, and the weights of these are the second operand of out^T = V^T w^T for the very same lane
 // if v's four positions stand there as the contraction index: nothing passes through LDS on the way.  The tiles of the cache hold
-// v in pieces of four positions x eight values for this: a lane's 128-bit load.
+// v in pieces of four positions x eight values for this: a lane's 128-bit load.  Scales and minima: sixteen lanes need those of eight
+// positions of k and of v, sixteen pairs; each lane loads and decodes one, and the others read it from its lane as they multiply.
 #include "device_common.h"
 #include "kv.h"
 #include "mfma.h"
@@ -22,17 +27,16 @@ namespace {
 
 // Below every score, and what a column's maximum is before it has seen one.
 constexpr float kLowest = -3.0e38f;
-// Weights times v's scales are brought below 2^12 by a power of two: binary16 then has all of its 11 bits down to 2^-26 of the largest.
-constexpr int kWeightTop = 12;
+// The weights are 2^unit larger than their definition, so that the largest one times the largest scale of v stays below 2^11 (binary16 has
+// all of its 11 bits down to 2^-25 of that), and below 2^15 while a column's maximum is up to 2^4 behind.
+constexpr int kWeightTop = 11;
+constexpr float kBehind = 4.0f;
 
-template <int D>
-__device__ __forceinline__ uint4 unpack_k(uint32_t w) {
-  const uint32_t h = w >> 8;
-  return make_uint4(w & 0x000F000Fu, w & 0x00F000F0u, h & 0x000F000Fu, h & 0x00F000F0u);
+// Codes of a word's halves as binary16 operands of 2^-20 each: values n and n + 4 of part n.
+__device__ __forceinline__ uint4 unpack_codes(uint32_t w) {
+  constexpr uint32_t kMask = 0x00F000F0u;
+  return make_uint4(w << 4 & kMask, w & kMask, w >> 4 & kMask, w >> 8 & kMask);
 }
-
-// 2^n for any n; what fp32 cannot hold is 0 or infinity.
-__device__ __forceinline__ float power_of_two(int n) { return ldexpf(1.0f, n); }
 
 __device__ __forceinline__ int clamp_int(int v, int low, int high) { return v < low ? low : v > high ? high : v; }
 
@@ -82,47 +86,93 @@ __device__ __forceinline__ Span seen_by(const AttentionArgs& a, const Tile& t, i
   return {low, high};
 }
 
-// Codes, scales and minima of two tiles of the cache, as a wave holds them.  Lane = 16 g + i: k's codes of position i, a quarter g of
-// its values; v's codes of positions 4 g .. 4 g + 3, eight values from 8 i on (a head of 64: from 8 (i % 8) on); scales and minima of
-// positions 4 g .. 4 g + 3.
+// Two tiles of the cache, as a wave holds them.  Lane = 16 g + i: k's codes of position i, a quarter g of its values; v's codes of positions
+// 4 g .. 4 g + 3, eight values from 8 i on (a head of 64: from 8 (i % 8) on); of the sixteen pairs (scale, minimum) that the lanes
+// 16 g .. 16 g + 15 use (positions 4 g .. 4 g + 3 of both tiles, k's, then v's) the i-th.
 template <int D>
-struct Step {
+struct Held {
   uint32_t k[2][D / 32];
-  uint4 v[2], k_params[2], v_params[2];
-  bool there[2];
+  uint4 v[2];
+  uint32_t pair;
+};
+
+// A request's pages of one cache head, and the two tiles of a step in them.
+struct Pages {
+  const __attribute__((address_space(4))) int32_t* table;
+  const uint8_t* head;
+  int last_tile;
+};
+struct Place {
+  const uint8_t* first;
+  const uint8_t* second;
+  uint32_t there;  // a bit each
+};
+// The pages of a step's tiles.  Tiles behind the last position are not looked up: the last one again, all of it hidden.
+struct Looked {
+  int first, second;
+};
+__device__ __forceinline__ Looked look_up(const AttentionArgs& a, const Pages& p, int step) {
+  const int tiles_log2 = a.at.page_shift - 4;
+  return {p.table[min(step * 2, p.last_tile) >> tiles_log2], p.table[min(step * 2 + 1, p.last_tile) >> tiles_log2]};
+}
+template <int D>
+__device__ __forceinline__ const uint8_t* find_tile(const AttentionArgs& a, const Pages& p, int tile, int page, bool& there) {
+  tile = min(tile, p.last_tile);
+  const int tiles_log2 = a.at.page_shift - 4;
+  there = page >= 0 && page < a.n_pages;
+  return p.head + (size_t)(uint32_t)(there ? page : 0) * a.at.page_stride + (uint32_t)(tile & ((1 << tiles_log2) - 1)) * (uint32_t)tile_bytes(D);
+}
+template <int D>
+__device__ __forceinline__ Place place_of(const AttentionArgs& a, const Pages& p, int step, const Looked& pages) {
+  bool one, two;
+  const uint8_t* first = find_tile<D>(a, p, step * 2, pages.first, one);
+  const uint8_t* second = find_tile<D>(a, p, step * 2 + 1, pages.second, two);
+  return {first, second, (one ? 1u : 0u) | (two ? 2u : 0u)};
+}
+// A lane's offsets in a tile.
+template <int D>
+struct Lane {
+  uint32_t k, v, pair;
+  bool second;  // its pair lies in the second tile
 };
 template <int D>
-__device__ __forceinline__ void load_step(const AttentionArgs& a, const int32_t* table, size_t head_offset, int step, int last_tile, int lane, Step<D>& s) {
-  const int g = lane >> 4, i = lane & 15;
+__device__ __forceinline__ Lane<D> offsets_of(int lane) {
+  const uint32_t g = (uint32_t)lane >> 4, i = (uint32_t)lane & 15;
+  return {i * (D / 2) + g * (D / 8), 8 * D + g * (2 * D) + (D == 128 ? i : i & 7) * 16, 16 * D + (i & 8) * 8 + g * 16 + (i & 3) * 4, (i & 4) != 0};
+}
+template <int D>
+__device__ __forceinline__ void load_k(const Place& at, const Lane<D>& lane, Held<D>& s) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    // tiles behind the last position are not looked up: the last one again, all of it hidden
-    const int tile = step * 2 + h < last_tile ? step * 2 + h : last_tile;
-    const int pos = tile * kTilePositions;
-    const int page = __builtin_amdgcn_readfirstlane(table[pos >> a.at.page_shift]);
-    s.there[h] = page >= 0 && page < a.n_pages;
-    const uint8_t* at = a.at.layer + (size_t)(s.there[h] ? page : 0) * a.at.page_stride + head_offset +
-                        (size_t)((pos & ((1 << a.at.page_shift) - 1)) / kTilePositions) * tile_bytes(D);
-    const uint8_t* k = at + i * (D / 2) + g * (D / 8);
+    const __amdgpu_buffer_rsrc_t tile = make_buffer(h ? at.second : at.first, tile_bytes(D));
     if constexpr (D == 128) {
-      const uint4 w = load128(k);
+      const uint4 w = buffer_load128<0>(tile, lane.k);
       s.k[h][0] = w.x, s.k[h][1] = w.y, s.k[h][2] = w.z, s.k[h][3] = w.w;
     } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(k);
+      const uint2 w = buffer_load64_at<0>(tile, lane.k, 0);
       s.k[h][0] = w.x, s.k[h][1] = w.y;
     }
-    s.v[h] = load128(at + 8 * D + g * (2 * D) + (D == 128 ? i : i & 7) * 16);
-    s.k_params[h] = load128(at + 16 * D + g * 16);
-    s.v_params[h] = load128(at + 16 * D + 64 + g * 16);
   }
+  const uint8_t *first = at.first, *second = at.second;
+  s.pair = *reinterpret_cast<const uint32_t*>((lane.second ? second : first) + (size_t)lane.pair);
+}
+template <int D>
+__device__ __forceinline__ void load_v(const Place& at, const Lane<D>& lane, Held<D>& s) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) s.v[h] = buffer_load128<0>(make_buffer(h ? at.second : at.first, tile_bytes(D)), lane.v);
 }
 
-// q of one column as the second operand of S^T = K q^T, times a power of two that brings its largest value to between 2^13 and 2^14;
-// the values that meet a nibble at 16 times its worth are a sixteenth.
+// The value of the i-th of a lane's sixteen neighbours.
+template <int I>
+__device__ __forceinline__ float of_lane(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x150 + I, 0xF, 0xF, true));
+}
+
+// q of one column as the second operand of S^T = K q^T, times a power of two that brings its largest value to between 2^13 and 2^14.
 template <int D>
 struct Query {
   uint4 parts[D / 32];
-  float sum;     // of the scaled values, times 2^-24 like the codes
+  float sum;     // of the scaled values, times 2^-20 like the codes
   float factor;  // from scores to powers of two
 };
 template <class DT, int D>
@@ -152,263 +202,421 @@ __device__ __forceinline__ void load_query(const AttentionArgs& a, const uint16_
   }
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
-  out.sum = sum * 0x1p-24f;
-  out.factor = fits ? ldexpf(a.scale * 1.44269504088896341f, 24 - up) : __uint_as_float(0x7FC00000u);
+  out.sum = sum * 0x1p-20f;
+  out.factor = fits ? ldexpf(a.scale * 1.44269504088896341f, 20 - up) : __uint_as_float(0x7FC00000u);
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
     const float* v = x + c * 8;
-    out.parts[c] = make_uint4(pack2<F16>(v[0], v[4]), pack2<F16>(v[1] * 0.0625f, v[5] * 0.0625f), pack2<F16>(v[2], v[6]),
-                              pack2<F16>(v[3] * 0.0625f, v[7] * 0.0625f));
+    out.parts[c] = make_uint4(pack2<F16>(v[0], v[4]), pack2<F16>(v[1], v[5]), pack2<F16>(v[2], v[6]), pack2<F16>(v[3], v[7]));
   }
 }
 
-// Codes of v of 32 positions as first operands of out^T = V^T w^T: of output tile j, row i of which is value 8 i + j of a head of
-// 128 and 8 (i % 8) + 4 (i / 8) + j of one of 64, j odd at 16 times their worth.
-template <int D>
-__device__ __forceinline__ void unpack_v(const uint4 (&v)[2], int lane, uint4 (&out)[D / 16]) {
-  const uint32_t pairs[4][2] = {{v[0].x, v[0].y}, {v[0].z, v[0].w}, {v[1].x, v[1].y}, {v[1].z, v[1].w}};
-  uint32_t w[D / 16][4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    // halves of the words of two positions side by side
-    const uint32_t own = D == 128 || (lane & 8) == 0 ? 0x05040100u : 0x07060302u;
-#pragma unroll
-    for (int h = 0; h < D / 64; ++h) {
-      const uint32_t both = __builtin_amdgcn_perm(pairs[e][1], pairs[e][0], h == 0 ? own : 0x07060302u), up = both >> 8;
-      w[h * 4][e] = both & 0x000F000Fu;
-      w[h * 4 + 1][e] = both & 0x00F000F0u;
-      w[h * 4 + 2][e] = up & 0x000F000Fu;
-      w[h * 4 + 3][e] = up & 0x00F000F0u;
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < D / 16; ++j) out[j] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
-}
-// First of the values whose row 4 g + i of tile j a lane receives: value_of + j.
+// First of the values whose row 4 g + i of output tile j a lane receives: value_of + j.
 template <int D>
 __device__ __forceinline__ int value_of(int row) {
   return D == 128 ? 8 * row : 8 * (row & 7) + 4 * (row >> 3);
 }
 
-// A column's softmax so far, in its lanes (each has a quarter of the positions' sums).
-struct Column {
-  float top;       // maximum of the scores in units of the column, the same in all of its lanes
-  float sum;       // of the weights
-  float minima;    // of the weights times v's minima
+// Two values as binary16, to the nearest even.
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
+}
+
+// A wave's columns: NT tiles of sixteen, a column's softmax in the four lanes that hold it (a quarter of the positions' sums each).
+template <int D, int NT>
+struct Columns {
+  Query<D> q[NT];
+  Span span[NT];     // of the lane's column
+  Span some, all;    // positions that some column of the wave sees, and that all do
+  float top[NT];     // maximum of the scores, up to kBehind of it behind, the same in all lanes of a column
+  float bar[NT];     // scores above it raise the maximum
+  float base[NT];    // 2^base: what a weight of 1 is worth
+  float sum[NT];     // of the weights
+  float minima[NT];  // of the weights times v's minima
+  f32x4 acc[NT][D / 16];  // of the weights times v's codes and scales, times 2^-20
+  int unit;
+  float limit;       // scales of v above it lower the unit; infinity in lanes that hold k's
 };
+template <int D, int NT>
+__device__ __forceinline__ void start_columns(Columns<D, NT>& c, int lane) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    c.top[n] = c.bar[n] = kLowest;
+    c.base[n] = c.sum[n] = c.minima[n] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) c.acc[n][j] = f32x4{};
+  }
+  c.unit = 100;
+  c.limit = lane & 8 ? 0.0f : __uint_as_float(0x7F800000u);
+}
 
-// Scores, weights and weighted values of 32 positions for one tile of sixteen columns.
-template <class DT, int D>
-__device__ __forceinline__ void attend_step(const Step<D>& s, const uint4 (&v_codes)[D / 16], const Query<D>& q, int first_pos, bool all_visible,
-                                            Span span, int lane, float v_unit, Column& col, f32x4 (&acc)[D / 16]) {
-  const int g = lane >> 4;
-  float x[8], v_scale[8], v_min[8];
+// Raises the columns' maxima to those of this step's scores and lowers the unit to its scales.
+template <int D, int NT>
+__device__ __forceinline__ void raise(Columns<D, NT>& c, const float (&highest)[NT], float scale, int lane) {
+  float s = lane & 8 ? scale : 0.0f;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    f32x4 dots = {};
+  for (int m = 1; m < 64; m <<= 1) s = fmaxf(s, __shfl_xor(s, m));
+  const int fits = min(kWeightTop - ((int)(__float_as_uint(s) >> 23) - 126), 100);  // s < 2^(kWeightTop - fits)
+  const int unit = min(c.unit, fits);
+  const float by = ldexpf(1.0f, unit - c.unit);
+  c.unit = unit;
+  if (lane & 8) c.limit = ldexpf(1.0f, kWeightTop - unit);
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) dots = mfma16x16x32<F16>(unpack_k<D>(s.k[h][c]), q.parts[c], dots);
-    const uint32_t kp[4] = {s.k_params[h].x, s.k_params[h].y, s.k_params[h].z, s.k_params[h].w};
-    const uint32_t vp[4] = {s.v_params[h].x, s.v_params[h].y, s.v_params[h].z, s.v_params[h].w};
+  for (int n = 0; n < NT; ++n) {
+    float top = fmaxf(highest[n], __shfl_xor(highest[n], 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    top = fmaxf(top, c.top[n]);
+    const float shrink = __builtin_amdgcn_exp2f((c.top[n] - top) * c.q[n].factor) * by;
+    c.top[n] = top;
+    c.bar[n] = top + kBehind / c.q[n].factor;
+    c.base[n] = fmaf(top, c.q[n].factor, -(float)unit);
+    c.sum[n] *= shrink;
+    c.minima[n] *= shrink;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float scale, low;
-      unpack2<DT>(kp[i], scale, low);
-      x[h * 4 + i] = fmaf(dots[i], scale, low * q.sum);
-      unpack2<DT>(vp[i], v_scale[h * 4 + i], v_min[h * 4 + i]);
-    }
-  }
-  uint32_t visible = 0xFFu;
-  if (!all_visible) {
-    visible = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int pos = first_pos + (e >> 2) * kTilePositions + g * 4 + (e & 3);
-      const bool sees = pos >= span.low && pos < span.high && s.there[e >> 2];
-      visible |= (uint32_t)sees << e;
-      if (!sees) x[e] = kLowest, v_min[e] = 0.0f, v_scale[e] = 0.0f;
-    }
-  }
-  float top = col.top;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
-  top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32));
-  if (__any(top > col.top)) {
-    const float shrink = __builtin_amdgcn_exp2f((col.top - top) * q.factor);
-    col.sum *= shrink;
-    col.minima *= shrink;
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) acc[j] *= shrink;
-    col.top = top;
-  }
-  const float base = col.top * q.factor;
-  float w[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    w[e] = __builtin_amdgcn_exp2f(fmaf(x[e], q.factor, -base));
-    if (!all_visible && !(visible >> e & 1u)) w[e] = 0.0f;
-    col.sum += w[e];
-    col.minima = fmaf(w[e], v_min[e], col.minima);
-    w[e] *= v_scale[e] * v_unit;
-  }
-  uint32_t high[4], low[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    high[e] = pack2<F16>(w[2 * e], w[2 * e + 1]);
-    if constexpr (std::is_same_v<DT, F16>) {
-      float a, b;
-      unpack2<F16>(high[e], a, b);
-      low[e] = pack2<F16>(w[2 * e] - a, w[2 * e + 1] - b);
-    }
-  }
-  const uint4 weights = make_uint4(high[0], high[1], high[2], high[3]);
-#pragma unroll
-  for (int j = 0; j < D / 16; ++j) acc[j] = mfma16x16x32<F16>(v_codes[j], weights, acc[j]);
-  if constexpr (std::is_same_v<DT, F16>) {
-    const uint4 rest = make_uint4(low[0], low[1], low[2], low[3]);
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) acc[j] = mfma16x16x32<F16>(v_codes[j], rest, acc[j]);
+    for (int j = 0; j < D / 16; ++j) c.acc[n][j] *= shrink;
   }
 }
 
-// v's scales are brought below 2^kWeightTop by a power of two of the wave's, which falls when a larger scale comes.  True if it fell; `by`: by
-// what the sums so far have to be multiplied.
-template <class DT, int D>
-__device__ __forceinline__ bool fit_scales(const Step<D>& s, int first_pos, bool all_visible, Span seen, int lane, float& limit, float& unit, float& by) {
-  float top = 0.0f;
+// What a step's scores are, and the scales and minima of its positions (a lane's own, see Held).
+template <int NT>
+struct Scores {
+  float x[NT][8], highest[NT];
+  uint32_t sees[NT];  // a bit for every position that the column sees
+  float scale, low, size;
+  bool above;         // of a bar or a limit: raise() is due
+};
+// Scores of the 32 positions whose keys are in `s`.  MASKED: some column does not see all of them, or a tile is not `there`.
+template <class DT, int D, int NT, bool MASKED>
+__device__ __forceinline__ void score_step(const Held<D>& s, int first_pos, uint32_t there, int lane, const Columns<D, NT>& c, Scores<NT>& r) {
+  const int g = lane >> 4, i = lane & 15;
+  // this lane's pair; v's odd positions from the top down
+  unpack2<DT>(s.pair, r.scale, r.low);
+  if (MASKED) {  // what nobody sees may hold anything
+    const int pos = first_pos + (i & 4) * 4 + g * 4 + (i & 3);
+    if (pos < c.some.low || pos >= c.some.high || !(there >> (i >> 2 & 1) & 1u)) r.scale = r.low = 0.0f;
+  }
+  r.size = r.scale;
+  const bool down = (i & 9) == 9;
+  r.low = fmaf(r.scale, down ? 15.0f : 0.0f, r.low);
+  r.scale = down ? -r.scale : r.scale;
+
+  f32x4 dots[NT][2] = {};
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint32_t vp[4] = {s.v_params[h].x, s.v_params[h].y, s.v_params[h].z, s.v_params[h].w};
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float scale, low;
-      unpack2<DT>(vp[i], scale, low);
-      if (!all_visible) {  // what nobody sees may hold anything
-        const int pos = first_pos + h * kTilePositions + (lane >> 4) * 4 + i;
-        if (pos < seen.low || pos >= seen.high || !s.there[h]) scale = 0.0f;
+    for (int w = 0; w < D / 32; ++w) {
+      const uint4 codes = unpack_codes(s.k[h][w]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) dots[n][h] = mfma16x16x32<F16>(codes, c.q[n].parts[w], dots[n][h]);
+    }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) r.highest[n] = kLowest, r.sees[n] = 0;
+  auto score = [&](auto which) {
+    constexpr int E = decltype(which)::value;
+    const float ks = of_lane<E>(r.scale), km = of_lane<E>(r.low);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float x = fmaf(dots[n][E >> 2][E & 3], ks, km * c.q[n].sum);
+      if (MASKED) {
+        const int pos = first_pos + (E >> 2) * kTilePositions + g * 4 + (E & 3);
+        const bool visible = pos >= c.span[n].low && pos < c.span[n].high && (there >> (E >> 2) & 1u);
+        r.sees[n] |= (uint32_t)visible << E;
+        x = visible ? x : kLowest;
       }
-      top = scale < __uint_as_float(0x7F800000u) ? fmaxf(top, scale) : top;
+      r.x[n][E] = x;
+      r.highest[n] = fmaxf(r.highest[n], x);
     }
-  }
-  if (!__any(top > limit)) return false;
+  };
+  score(std::integral_constant<int, 0>{}), score(std::integral_constant<int, 1>{}), score(std::integral_constant<int, 2>{});
+  score(std::integral_constant<int, 3>{}), score(std::integral_constant<int, 4>{}), score(std::integral_constant<int, 5>{});
+  score(std::integral_constant<int, 6>{}), score(std::integral_constant<int, 7>{});
+  if (!MASKED && there != 3) {  // a page that is not of the cache
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-  const int exponent = (int)(__float_as_uint(top) >> 23) - 127 + 1;  // top < 2^exponent
-  const int up = min(kWeightTop - exponent, 100);
-  const float to = power_of_two(up);
-  by = to / unit;
-  unit = to;
-  limit = power_of_two(kWeightTop - up);
-  return true;
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (!(there >> (e >> 2) & 1u)) r.x[n][e] = -__uint_as_float(0x7F800000u);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      r.highest[n] = r.x[n][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) r.highest[n] = fmaxf(r.highest[n], r.x[n][e]);
+    }
+    if (!(there >> (i >> 2 & 1) & 1u)) r.scale = r.low = r.size = 0.0f;
+  }
+  r.above = r.size > c.limit;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) r.above |= r.highest[n] > c.bar[n];
 }
 
-// Sixteen columns of one cache head: the four waves take steps of 32 positions in turn and meet in LDS.  grid = (cache heads x tiles, slices).
-template <class DT, int D>
-__global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a, int first_tile) {
-  __shared__ float sums[4][16][D + 4];
-  __shared__ float4 stats[4][16];  // maximum in powers of two, sum of weights, of weights times minima
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const int head = blockIdx.x % a.at.n_kv_heads, tile = first_tile + blockIdx.x / a.at.n_kv_heads, slice = blockIdx.y;
-  Tile t;
-  if (!tile_of_batch(a, 4, tile, t)) return;
-  const int column = t.first_column + c;
-  const bool live = column < t.columns;
-  const int row = live ? column / a.group : 0;
-  const int q_head = head * a.group + (live ? column - row * a.group : 0);
-  const int last_column = min(t.first_column + 15, t.columns - 1);
-  const Span first = seen_by(a, t, t.first_column / a.group), last = seen_by(a, t, last_column / a.group);
-  const Span span = live ? seen_by(a, t, row) : Span{first.low, last.high};
-  // steps of this slice, then this wave's of them
-  const int from = first.low / kStepPositions;
-  const int steps = last.high > first.low ? (last.high + kStepPositions - 1) / kStepPositions - from : 0;
-  const int per = max(a.slice_steps, (steps + a.slices - 1) / a.slices);
-  const int begin = from + min(steps, slice * per), end = from + min(steps, (slice + 1) * per);
+// Weights of a step and the weighted values.
+template <class DT, int D, int NT, bool MASKED>
+__device__ __forceinline__ void weigh_step(const Held<D>& s, int lane, Scores<NT>& r, Columns<D, NT>& c) {
+  constexpr bool kTwoParts = std::is_same_v<DT, F16>;
+  uint32_t high[NT][4], rest[NT][4];
+  auto weigh = [&](auto which) {
+    constexpr int E = decltype(which)::value;
+    const float vs = of_lane<8 + E>(r.scale), vm = of_lane<8 + E>(r.low);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const bool visible = !MASKED || (r.sees[n] >> E & 1u);
+      const float w = visible ? __builtin_amdgcn_exp2f(fmaf(r.x[n][E], c.q[n].factor, -c.base[n])) : 0.0f;
+      c.sum[n] += w;
+      c.minima[n] = fmaf(w, visible ? vm : 0.0f, c.minima[n]);
+      r.x[n][E] = w * (visible ? vs : 0.0f);
+      if constexpr (E & 1) {
+        high[n][E / 2] = pack_half(r.x[n][E - 1], r.x[n][E]);
+        if constexpr (kTwoParts) {
+          float a, b;
+          unpack2<F16>(high[n][E / 2], a, b);
+          rest[n][E / 2] = pack_half(r.x[n][E - 1] - a, r.x[n][E] - b);
+        }
+      }
+    }
+  };
+  weigh(std::integral_constant<int, 0>{}), weigh(std::integral_constant<int, 1>{}), weigh(std::integral_constant<int, 2>{});
+  weigh(std::integral_constant<int, 3>{}), weigh(std::integral_constant<int, 4>{}), weigh(std::integral_constant<int, 5>{});
+  weigh(std::integral_constant<int, 6>{}), weigh(std::integral_constant<int, 7>{});
 
-  Query<D> q;
-  const long long at = t.first_row + row;
-  load_query<DT, D>(a, a.q + at * a.q_stride + q_head * D, live, lane, q);
-  Column col = {kLowest, 0.0f, 0.0f};
-  f32x4 acc[D / 16] = {};
-  float limit = 0.0f, unit = power_of_two(100);
-  const int32_t* table = a.tables + (size_t)t.request * a.table_width;
-  const size_t head_offset = (size_t)head * ((1u << a.at.page_shift) / kTilePositions) * tile_bytes(D);
-  const int last_tile = (last.high - 1) / kTilePositions;
-  for (int s = begin + wave; s < end; s += 4) {
-    Step<D> step;
-    load_step<D>(a, table, head_offset, s, last_tile, lane, step);
-    const int pos = s * kStepPositions;
-    const bool all_visible = pos >= last.low && pos + kStepPositions <= first.high && step.there[0] && step.there[1];
-    float by;
-    if (fit_scales<DT, D>(step, pos, all_visible, Span{first.low, last.high}, lane, limit, unit, by)) {
+  // v's codes as first operands of out^T = V^T w^T: row i of output tile j is value 8 i + j of a head of 128, 8 (i % 8) + 4 (i / 8) + j of
+  // one of 64; halves of the words of two positions side by side
+  const uint32_t pairs[4][2] = {{s.v[0].x, ~s.v[0].y}, {s.v[0].z, ~s.v[0].w}, {s.v[1].x, ~s.v[1].y}, {s.v[1].z, ~s.v[1].w}};
+  const uint32_t own = D == 128 || (lane & 8) == 0 ? 0x05040100u : 0x07060302u;
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) acc[j] *= by;
+  for (int h = 0; h < D / 64; ++h) {
+    uint4 parts[4];  // of a pair of positions each: tiles 4 h .. 4 h + 3
+#pragma unroll
+    for (int e = 0; e < 4; ++e) parts[e] = unpack_codes(__builtin_amdgcn_perm(pairs[e][1], pairs[e][0], h == 0 ? own : 0x07060302u));
+    const uint4 codes[4] = {make_uint4(parts[0].x, parts[1].x, parts[2].x, parts[3].x), make_uint4(parts[0].y, parts[1].y, parts[2].y, parts[3].y),
+                            make_uint4(parts[0].z, parts[1].z, parts[2].z, parts[3].z), make_uint4(parts[0].w, parts[1].w, parts[2].w, parts[3].w)};
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const uint4 weights = make_uint4(high[n][0], high[n][1], high[n][2], high[n][3]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c.acc[n][h * 4 + j] = mfma16x16x32<F16>(codes[j], weights, c.acc[n][h * 4 + j]);
+      if constexpr (kTwoParts) {
+        const uint4 more = make_uint4(rest[n][0], rest[n][1], rest[n][2], rest[n][3]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c.acc[n][h * 4 + j] = mfma16x16x32<F16>(codes[j], more, c.acc[n][h * 4 + j]);
+      }
     }
-    uint4 v_codes[D / 16];
-    unpack_v<D>(step.v, lane, v_codes);
-    attend_step<DT, D>(step, v_codes, q, pos, all_visible, span, lane, unit, col, acc);
   }
-  col.sum += __shfl_xor(col.sum, 16);
-  col.sum += __shfl_xor(col.sum, 32);
-  col.minima += __shfl_xor(col.minima, 16);
-  col.minima += __shfl_xor(col.minima, 32);
-  if (live) {
-    const float back = 1.0f / unit;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) sums[wave][c][value_of<D>(4 * g + i) + j] = acc[j][i] * (j & 1 ? 0x1p20f : 0x1p24f) * back;
+}
+
+// The next step's keys are loaded as soon as the scores are there, its values after the products with this one's.
+template <class DT, int D, int NT>
+__device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages& p, int begin, int end, int stride_log2, int lane, Columns<D, NT>& c) {
+  if (begin >= end) return;
+  const Lane<D> offsets = offsets_of<D>(lane);
+  // of the wave's steps, begin + (n << stride_log2), those from the head'th to the tail'th are seen whole by all columns; the others come first
+  const int stride = 1 << stride_log2, count = (end - begin + stride - 1) >> stride_log2;
+  auto steps_before = [&](int step) { return clamp_int((step - begin + stride - 1) >> stride_log2, 0, count); };
+  const int head = steps_before((c.all.low + kStepPositions - 1) / kStepPositions), tail = max(steps_before(c.all.high / kStepPositions), head);
+  const int ends = head + count - tail;
+  auto step_at = [&](int n) { return begin + ((n < head ? n : n < ends ? n - head + tail : n - ends + head) << stride_log2); };
+  Held<D> held;
+  // pages are looked up two steps ahead of their use: a scalar load's wait is for all of them
+  Looked pages = look_up(a, p, step_at(1));
+  Place at = place_of<D>(a, p, step_at(0), look_up(a, p, step_at(0))), next;
+  load_k<D>(at, offsets, held);
+  load_v<D>(at, offsets, held);
+  next = place_of<D>(a, p, step_at(1), pages);
+  pages = look_up(a, p, step_at(2));
+  int n = 0;
+  auto on = [&] {
+    ++n;
+    at = next;
+    next = place_of<D>(a, p, step_at(n + 1), pages);
+    pages = look_up(a, p, step_at(n + 2));
+  };
+  Scores<NT> r;
+  while (n < ends) {
+    score_step<DT, D, NT, true>(held, step_at(n) * kStepPositions, at.there, lane, c, r);
+    load_k<D>(next, offsets, held);
+    if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
+    weigh_step<DT, D, NT, true>(held, lane, r, c);
+    load_v<D>(next, offsets, held);
+    on();
+  }
+  while (n < count) {
+    // raise() stands outside of the inner loop, and the step is begun again for it: inside, the sums would be copied at every step
+    score_step<DT, D, NT, false>(held, 0, at.there, lane, c, r);
+    if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
+    for (;;) {
+      load_k<D>(next, offsets, held);
+      weigh_step<DT, D, NT, false>(held, lane, r, c);
+      load_v<D>(next, offsets, held);
+      on();
+      if (n >= count) break;
+      score_step<DT, D, NT, false>(held, 0, at.there, lane, c, r);
+      if (__any(r.above)) break;
     }
-    if (g == 0) stats[wave][c] = make_float4(col.top == kLowest ? kLowest : col.top * q.factor, col.sum, col.minima, 0.0f);
   }
-  __syncthreads();
-  // sixteen threads to a column
-  const int mine = threadIdx.x >> 4, part = threadIdx.x & 15;
-  if (t.first_column + mine >= t.columns) return;
-  float top = kLowest;
+}
+
+// A wave's columns, from column `first` of the request on, and the steps [from, from + steps) of this slice that they look at.
+struct Steps {
+  int begin, end;
+};
+template <class DT, int D, int NT>
+__device__ __forceinline__ Steps load_columns(const AttentionArgs& a, const Tile& t, int first, int head, int slice, int lane, Columns<D, NT>& c, Pages& p) {
+  start_columns<D, NT>(c, lane);
+  const int last_column = min(first + 16 * NT, t.columns) - 1;
+  const Span lowest = seen_by(a, t, first / a.group), highest = seen_by(a, t, last_column / a.group);
+  c.some = {lowest.low, highest.high};
+  c.all = {highest.low, lowest.high};
 #pragma unroll
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[w][mine].x);
-  float weight[4], sum = 0.0f, minima = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    weight[w] = __builtin_amdgcn_exp2f(stats[w][mine].x - top);
-    sum += weight[w] * stats[w][mine].y;
-    minima += weight[w] * stats[w][mine].z;
+  for (int n = 0; n < NT; ++n) {
+    const int column = first + n * 16 + (lane & 15);
+    const bool live = column < t.columns;
+    const int row = live ? column / a.group : 0, of_group = live ? column - row * a.group : 0;
+    c.span[n] = live ? seen_by(a, t, row) : c.some;
+    load_query<DT, D>(a, a.q + (long long)(t.first_row + row) * a.q_stride + (head * a.group + of_group) * D, live, lane, c.q[n]);
   }
-  const int my_row = (t.first_column + mine) / a.group, my_head = head * a.group + (t.first_column + mine) - my_row * a.group;
-  const long long out_row = t.first_row + my_row;
-  constexpr int PER = D / 16;
-  float v[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    v[i] = minima;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) v[i] = fmaf(weight[w], sums[w][mine][part * PER + i], v[i]);
-  }
+  p.table = (const __attribute__((address_space(4))) int32_t*)(a.tables + (size_t)t.request * a.table_width);
+  p.head = a.at.layer + (size_t)head * ((1u << a.at.page_shift) / kTilePositions) * tile_bytes(D);
+  p.last_tile = (c.some.high - 1) / kTilePositions;
+  const int from = c.some.low / kStepPositions;
+  const int steps = c.some.high > c.some.low ? (c.some.high + kStepPositions - 1) / kStepPositions - from : 0;
+  const int per = max(a.slice_steps, (steps + a.slices - 1) / a.slices);
+  return {from + min(steps, slice * per), from + min(steps, (slice + 1) * per)};
+}
+
+// Sums of a column over its four lanes.
+__device__ __forceinline__ float of_column(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+__device__ __forceinline__ float log_sum(float base, float sum) {
+  return sum == 0.0f ? -__uint_as_float(0x7F800000u) : (base + log2f(sum)) * 0.693147180559945309f;
+}
+
+// Output of a column's values from `value` on: v unnormalised.
+template <class DT, int D, int N>
+__device__ __forceinline__ void put_values(const AttentionArgs& a, long long row, int q_head, int slice, int value, const float (&v)[N], float sum, float inverse) {
   if (a.slices > 1) {
-    const size_t to = ((size_t)out_row * a.n_heads + my_head) * a.slices + slice;
+    const size_t part = ((size_t)row * a.n_heads + q_head) * a.slices + slice;
 #pragma unroll
-    for (int i = 0; i < PER; i += 4) *reinterpret_cast<float4*>(a.sums + to * D + part * PER + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    if (part == 0) a.tops[to] = make_float2(top, sum);
+    for (int k = 0; k < N; k += 4) *reinterpret_cast<float4*>(a.sums + part * D + value + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
     return;
   }
-  const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint32_t packed[PER / 2];
+  uint2* to = reinterpret_cast<uint2*>(a.out + row * a.out_stride + q_head * D + value);
 #pragma unroll
-  for (int i = 0; i < PER; i += 2) packed[i / 2] = pack2<DT>(sum == 0.0f ? 0.0f : v[i] * inverse, sum == 0.0f ? 0.0f : v[i + 1] * inverse);
-  uint32_t* to = reinterpret_cast<uint32_t*>(a.out + out_row * a.out_stride + my_head * D + part * PER);
+  for (int k = 0; k < N; k += 4) {
+    float w[4];
 #pragma unroll
-  for (int i = 0; i < PER / 2; ++i) to[i] = packed[i];
-  if (a.lse != nullptr && part == 0)
-    a.lse[out_row * a.n_heads + my_head] = sum == 0.0f ? -__uint_as_float(0x7F800000u) : (top + log2f(sum)) * 0.693147180559945309f;
+    for (int e = 0; e < 4; ++e) w[e] = sum == 0.0f ? 0.0f : v[k + e] * inverse;
+    to[k / 4] = make_uint2(pack2<DT>(w[0], w[1]), pack2<DT>(w[2], w[3]));
+  }
+}
+__device__ __forceinline__ void put_sum(const AttentionArgs& a, long long row, int q_head, int slice, float base, float sum) {
+  const size_t item = (size_t)row * a.n_heads + q_head;
+  if (a.slices > 1)
+    a.tops[item * a.slices + slice] = make_float2(base, sum);
+  else if (a.lse != nullptr)
+    a.lse[item] = log_sum(base, sum);
 }
 
-// Joins the slices of a row's head, a wave each.  grid = rows x heads / 4.
+// What the waves of a workgroup that share columns hand to one another.
+template <int D, int NT>
+struct Shared {
+  float sums[4][16 * NT][D + 4];
+  float4 stats[4][16 * NT];  // worth of a weight of 1 in powers of two, sum of weights, of weights times minima
+};
+
+// A tile's columns, 16 NT to a wave; where they are fewer than the waves, 2 or 4 waves take the same ones and the steps in turn.
+template <class DT, int D, int NT>
+__device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& t, int columns, int head, int slice, Shared<D, NT>& shared) {
+  constexpr int PER = 16 * NT;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
+  const int groups_log2 = columns <= PER ? 0 : columns <= 2 * PER ? 1 : 2, group = wave & ((1 << groups_log2) - 1);
+  const int first = t.first_column + group * PER;
+  Columns<D, NT> c;
+  if (first < t.columns) {
+    Pages p;
+    const Steps steps = load_columns<DT, D, NT>(a, t, first, head, slice, lane, c, p);
+    attend_steps<DT, D, NT>(a, p, steps.begin + (wave >> groups_log2), steps.end, 2 - groups_log2, lane, c);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float sum = of_column(c.sum[n]), minima = of_column(c.minima[n]);
+      const float base = c.top[n] == kLowest ? kLowest : c.base[n], inverse = 1.0f / sum;
+      const int column = first + n * 16 + i;
+      if (column >= t.columns) continue;
+      const int row = column / a.group, q_head = head * a.group + column - row * a.group;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int value = value_of<D>(4 * g + r);
+        float v[D / 16];
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) v[j] = c.acc[n][j][r] * 0x1p20f;
+        if (groups_log2 < 2) {
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) shared.sums[wave][n * 16 + i][value + j] = v[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) v[j] += minima;
+          put_values<DT, D>(a, t.first_row + row, q_head, slice, value, v, sum, inverse);
+        }
+      }
+      if (g != 0) continue;
+      if (groups_log2 < 2)
+        shared.stats[wave][n * 16 + i] = make_float4(base, sum, minima, 0.0f);
+      else
+        put_sum(a, t.first_row + row, q_head, slice, base, sum);
+    }
+  }
+  if (groups_log2 == 2) return;
+  __syncthreads();
+  // sixteen threads to a column
+  const int waves = 4 >> groups_log2, part = threadIdx.x & 15;
+  for (int of_tile = threadIdx.x >> 4; of_tile < columns; of_tile += 16) {
+    const int from = of_tile / PER, at = of_tile % PER;
+    float base = kLowest;
+    for (int w = 0; w < waves; ++w) base = fmaxf(base, shared.stats[(w << groups_log2) + from][at].x);
+    float sum = 0.0f, minima = 0.0f, v[D / 16] = {};
+    for (int w = 0; w < waves; ++w) {
+      const int of = (w << groups_log2) + from;
+      const float4 stat = shared.stats[of][at];
+      const float weight = __builtin_amdgcn_exp2f(stat.x - base);
+      sum = fmaf(weight, stat.y, sum);
+      minima = fmaf(weight, stat.z, minima);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) v[k] = fmaf(weight, shared.sums[of][at][part * (D / 16) + k], v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) v[k] += minima;
+    const int column = t.first_column + of_tile, row = column / a.group, q_head = head * a.group + column - row * a.group;
+    put_values<DT, D>(a, t.first_row + row, q_head, slice, part * (D / 16), v, sum, 1.0f / sum);
+    if (part == 0) put_sum(a, t.first_row + row, q_head, slice, base, sum);
+  }
+}
+
+// 2^COLUMNS_LOG2 columns of one cache head, 16 (few) or 64 NT of them.  grid = (cache heads x tiles, slices); the last tiles, which see most,
+// first.
+template <class DT, int D, int NT, int COLUMNS_LOG2>
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_kernel(AttentionArgs a, int first_tile, int tiles) {
+  __shared__ Shared<D, NT> shared;
+  const int head = blockIdx.x % a.at.n_kv_heads, tile = first_tile + tiles - 1 - (int)(blockIdx.x / a.at.n_kv_heads), slice = blockIdx.y;
+  Tile t;
+  if (!tile_of_batch(a, COLUMNS_LOG2, tile, t)) return;
+  const int columns = min(t.columns - t.first_column, 1 << COLUMNS_LOG2);
+  if (NT > 1 && columns <= 16)
+    attend_tile<DT, D, 1>(a, t, columns, head, slice, reinterpret_cast<Shared<D, 1>&>(shared));
+  else
+    attend_tile<DT, D, NT>(a, t, columns, head, slice, shared);
+}
+
+// Joins the slices of a row's head: D / 4 threads take four values each, the others of the workgroup other slices.  grid = rows x heads.
 template <class DT, int D>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, long long first) {
-  const long long item = first + (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (item >= (long long)a.n_tokens * a.n_heads) return;
+  constexpr int THREADS = D / 4, GROUPS = 256 / THREADS;
+  __shared__ float4 parts[GROUPS][THREADS];
+  __shared__ float sums[GROUPS];
+  const long long item = first + blockIdx.x;
+  const int lane = threadIdx.x & 63, part = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
   const int row = (int)(item / a.n_heads), head = (int)(item - (long long)row * a.n_heads);
   if (row < a.q_starts[0] || row >= a.q_starts[a.n_reqs]) return;
   const float2* tops = a.tops + item * a.slices;
@@ -416,32 +624,40 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, lo
   for (int z = lane; z < a.slices; z += 64) top = fmaxf(top, tops[z].x);
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-  constexpr int PER = D / 64;
-  float v[PER] = {}, sum = 0.0f;
-  for (int z = 0; z < a.slices; ++z) {
-    const float2 p = tops[z];
-    if (p.y == 0.0f) continue;  // a slice without positions
-    const float w = __builtin_amdgcn_exp2f(p.x - top);
-    sum += w * p.y;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = fmaf(w, a.sums[(item * a.slices + z) * D + lane * PER + i], v[i]);
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int z = group; z < a.slices; z += GROUPS) {
+    const float2 of = tops[z];
+    const float4 x = *reinterpret_cast<const float4*>(a.sums + (item * a.slices + z) * D + part * 4);
+    const float w = __builtin_amdgcn_exp2f(of.x - top);
+    sum = fmaf(w, of.y, sum);
+    v.x = fmaf(w, x.x, v.x), v.y = fmaf(w, x.y, v.y), v.z = fmaf(w, x.z, v.z), v.w = fmaf(w, x.w, v.w);
+  }
+  parts[group][part] = v;
+  if (part == 0) sums[group] = sum;
+  __syncthreads();
+  if (group != 0) return;
+  for (int k = 1; k < GROUPS; ++k) {
+    const float4 x = parts[k][part];
+    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+    sum += sums[k];
   }
   const float inverse = 1.0f / sum;
-  uint16_t* to = a.out + (long long)row * a.out_stride + head * D + lane * PER;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) to[i] = (uint16_t)encode1<DT>(sum == 0.0f ? 0.0f : v[i] * inverse);
-  if (a.lse != nullptr && lane == 0)
-    a.lse[item] = sum == 0.0f ? -__uint_as_float(0x7F800000u) : (top + log2f(sum)) * 0.693147180559945309f;
+  const bool none = sum == 0.0f;
+  *reinterpret_cast<uint2*>(a.out + (long long)row * a.out_stride + head * D + part * 4) =
+      make_uint2(none ? 0 : pack2<DT>(v.x * inverse, v.y * inverse), none ? 0 : pack2<DT>(v.z * inverse, v.w * inverse));
+  if (a.lse != nullptr && part == 0) a.lse[item] = log_sum(top, sum);
 }
 
-template <class DT, int D>
-hipError_t few_typed(const AttentionArgs& a, hipStream_t st) {
-  const long long tiles = attention_tiles(a.n_tokens, a.group, a.n_reqs, kFewColumns);
-  // fewer than 2^31 threads to a launch
+// Launches over ranges of tiles, fewer than 2^31 threads each.
+template <class F>
+hipError_t by_tiles(const AttentionArgs& a, int columns, F launch) {
+  const long long tiles = attention_tiles(a.n_tokens, a.group, a.n_reqs, columns);
   const long long share = (1LL << 30) / 256 / a.slices / a.at.n_kv_heads, most = share > 0 ? share : 1;
   for (long long first = 0; first < tiles; first += most) {
     const long long n = tiles - first < most ? tiles - first : most;
-    attention_few_kernel<DT, D><<<dim3((unsigned)(n * a.at.n_kv_heads), (unsigned)a.slices), 256, 0, st>>>(a, (int)first);
+    launch(dim3((unsigned)(n * a.at.n_kv_heads), (unsigned)a.slices), (int)first, (int)n);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
@@ -449,11 +665,23 @@ hipError_t few_typed(const AttentionArgs& a, hipStream_t st) {
 }
 
 template <class DT, int D>
+hipError_t columns_typed(const AttentionArgs& a, hipStream_t st) {
+  return by_tiles(a, a.columns, [&](dim3 grid, int first, int n) {
+    if (a.columns == kFewColumns)
+      attention_kernel<DT, D, 1, 4><<<grid, 256, 0, st>>>(a, first, n);
+    else if (a.columns == kSomeColumns)
+      attention_kernel<DT, D, 1, 6><<<grid, 256, 0, st>>>(a, first, n);
+    else
+      attention_kernel<DT, D, 2, 7><<<grid, 256, 0, st>>>(a, first, n);
+  });
+}
+
+template <class DT, int D>
 hipError_t join_typed(const AttentionArgs& a, hipStream_t st) {
-  const long long items = (long long)a.n_tokens * a.n_heads, most = 1LL << 24;
+  const long long items = (long long)a.n_tokens * a.n_heads, most = 1LL << 22;
   for (long long first = 0; first < items; first += most) {
     const long long n = items - first < most ? items - first : most;
-    attention_join_kernel<DT, D><<<(unsigned)((n + 3) / 4), 256, 0, st>>>(a, first);
+    attention_join_kernel<DT, D><<<(unsigned)n, 256, 0, st>>>(a, first);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
@@ -462,9 +690,9 @@ hipError_t join_typed(const AttentionArgs& a, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_attention_few(const AttentionArgs& a, hipStream_t st) {
-  if (a.bf16) return a.at.head_dim == 64 ? few_typed<BF16, 64>(a, st) : few_typed<BF16, 128>(a, st);
-  return a.at.head_dim == 64 ? few_typed<F16, 64>(a, st) : few_typed<F16, 128>(a, st);
+hipError_t launch_attention(const AttentionArgs& a, hipStream_t st) {
+  if (a.bf16) return a.at.head_dim == 64 ? columns_typed<BF16, 64>(a, st) : columns_typed<BF16, 128>(a, st);
+  return a.at.head_dim == 64 ? columns_typed<F16, 64>(a, st) : columns_typed<F16, 128>(a, st);
 }
 
 hipError_t launch_attention_join(const AttentionArgs& a, hipStream_t st) {
