@@ -579,13 +579,13 @@ int sgmv_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t la
                       int32_t n_heads, int64_t out_stride, int64_t q_stride, float scale, int32_t causal, int32_t window, void* workspace,
                       size_t workspace_bytes, void* stream);
 
-/* Workspace that sgmv_attention_q4 would like for such a batch (its hints included); 0 where none helps.  Host-only. */
-size_t sgmv_attention_workspace_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads);
+/* Workspace that sgmv_attention_q4 would like for such a batch (its hints included) and window; 0 where none helps.  Host-only. */
+size_t sgmv_attention_workspace_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, int32_t window);
 
 /* Host-only, pure: what sgmv_attention_q4 would launch (`slices` = parts of a request's positions; with more than one a second launch
  * joins them).  Returns the status that the call's sizes alone give. */
-int sgmv_plan_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, const void* workspace, size_t workspace_bytes,
-                           sgmv_plan* plan);
+int sgmv_plan_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, int32_t window, const void* workspace,
+                           size_t workspace_bytes, sgmv_plan* plan);
 
 /* Measurement aid, not part of the operator: enqueue one plain kernel of known traffic on
  * `stream`, for the benchmark's attainable-bandwidth figure and for scaling a profiler's HBM

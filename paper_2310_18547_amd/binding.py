@@ -174,9 +174,9 @@ def _load():
     L.sgmv_attention_q4.argtypes = [C, KB, c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p, c.c_int32, c.c_int64, c.c_int64, c.c_float,
                                     c.c_int32, c.c_int32, c.c_void_p, c.c_size_t, c.c_void_p]
     L.sgmv_attention_q4.restype = c.c_int
-    L.sgmv_attention_workspace_bytes.argtypes = [C, KB, c.c_int32]
+    L.sgmv_attention_workspace_bytes.argtypes = [C, KB, c.c_int32, c.c_int32]
     L.sgmv_attention_workspace_bytes.restype = c.c_size_t
-    L.sgmv_plan_attention_q4.argtypes = [C, KB, c.c_int32, c.c_void_p, c.c_size_t, c.POINTER(SgmvPlan)]
+    L.sgmv_plan_attention_q4.argtypes = [C, KB, c.c_int32, c.c_int32, c.c_void_p, c.c_size_t, c.POINTER(SgmvPlan)]
     L.sgmv_plan_attention_q4.restype = c.c_int
     L.sgmv_probe.argtypes = [c.c_int, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
     L.sgmv_probe.restype = c.c_int
@@ -239,8 +239,8 @@ def sgmv_kv_page_bytes(cache: SgmvKvCache) -> int:
     return int(lib.sgmv_kv_page_bytes(ctypes.byref(cache)))
 
 
-def sgmv_attention_workspace_bytes(cache: SgmvKvCache, batch: SgmvKvBatch, n_heads: int) -> int:
-    return int(lib.sgmv_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads))
+def sgmv_attention_workspace_bytes(cache: SgmvKvCache, batch: SgmvKvBatch, n_heads: int, window: int = 0) -> int:
+    return int(lib.sgmv_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), n_heads, window))
 
 
 def sgmv_status_string(status: int) -> str:
@@ -401,11 +401,11 @@ def _calls():
  sgmv_attention_q4) = _calls()
 
 
-def sgmv_plan_attention_q4(cache: SgmvKvCache, batch: SgmvKvBatch, n_heads: int, workspace=None, workspace_bytes: int = 0,
-                           check: bool = True):
+def sgmv_plan_attention_q4(cache: SgmvKvCache, batch: SgmvKvBatch, n_heads: int, window: int = 0, workspace=None,
+                           workspace_bytes: int = 0, check: bool = True):
     """Host-only: the ``SgmvPlan`` of a ``sgmv_attention_q4`` call (``check=False``: ``(status, plan)``)."""
     plan = SgmvPlan()
-    rc = lib.sgmv_plan_attention_q4(ctypes.byref(cache), ctypes.byref(batch), n_heads, _addr(workspace), workspace_bytes,
+    rc = lib.sgmv_plan_attention_q4(ctypes.byref(cache), ctypes.byref(batch), n_heads, window, _addr(workspace), workspace_bytes,
                                     ctypes.byref(plan))
     if not check:
         return rc, plan

@@ -80,6 +80,7 @@ struct AttentionArgs {
   const int32_t* q_starts;
   const int32_t* kv_lens;
   const int32_t* tables;
+  float classes;             // classes of lengths for a position (request_by_length)
   int slices;                // parts of a tile's positions (workgroups), joined by a second launch where there are several
   int slice_steps;           // steps of a slice at least
   float* sums;               // slices > 1: [n_tokens][n_heads][slices][head_dim] unnormalised, then ...

@@ -13,11 +13,8 @@ using namespace sgmv;
 
 // Most heads, and most positions that a request's block table covers.
 constexpr int kMostHeads = 1 << 16, kMostPositions = 1 << 30;
-// Smallest slice of a request's positions that is worth a workgroup of its own: a step for each of its waves.
-constexpr int kSliceSteps = 4;
-// Workgroups per compute unit that slicing aims at.
-constexpr int kGroupsPerUnit = 4;
-
+// Most parts of a request's positions.
+constexpr int kMostSlices = 256;
 int check_cache(const sgmv_kv_cache* c) {
   if (c == nullptr) return SGMV_ERR_NULL;
   if (c->dtype != SGMV_F16 && c->dtype != SGMV_BF16) return SGMV_ERR_UNSUPPORTED;
@@ -95,30 +92,66 @@ struct AttentionPlan {
 size_t slice_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads) {
   return (size_t)b->n_tokens * (size_t)n_heads * (4 * (size_t)c->head_dim + 8);
 }
-// Columns of a workgroup for requests of so many rows.
-int columns_of(const sgmv_kv_batch* b, int32_t n_kv_heads, long long group, long long rows) {
-  if (rows * group <= kFewColumns) return kFewColumns;
-  return attention_tiles(b->n_tokens, (int)group, b->n_reqs, kManyColumns) * n_kv_heads >= 4LL * compute_units() || rows * group <= 32 ? kManyColumns : kSomeColumns;
-}
+// Time of an attention launch in us, to choose the kernel and the slices by.  One, two and three workgroups to a unit take 1.2, 1.6 and 2.4 us for a step
+// of 32 positions of sixteen columns (the loads; 131 000 positions in 48, 64 and 96 slices: 1.5, 1.8, 2.4), 1.4 where the keys come from the
+// caches, and 1.6 for thirty-two columns to a wave; a workgroup's lookups, queries and end take 4 us (64 requests of 512 to 2048 positions, 32
+// heads: 80 us whole, 133 in six slices), and a batch's last round is half empty; a join 3 us and its sums' way there and back at 4 TB/s.
+struct Estimate {
+  double steps, mean_steps;  // of the longest tile, and of an average one
+  double rows, heads, tile_bytes, units;
+  // workgroups of a slice; waves of a workgroup that share the steps, in a tile of the longest request and in an average one
+  double us(int columns, double groups, double share, double mean_share, int slices) const {
+    const double resident = columns == kManyColumns ? 2 : 3, total = groups * slices, slots = resident * units;
+    const int waves = total >= slots ? (int)resident : (int)((total + units - 1) / units);
+    const double step = columns == kFewColumns ? (waves == 1 ? 1.2 : waves == 2 ? 1.6 : 2.4) : columns == kSomeColumns ? 1.4 : 1.6;
+    const double longest = (double)(long long)(steps / slices / share + 0.999) * step + 4.0;
+    const double all = total > slots ? (total / slots + 0.5) * (mean_steps / slices / mean_share * step + 4.0) : 0.0;
+    return 1.5 + (longest > all ? longest : all) + (slices > 1 ? 3.0 + rows * heads * slices * tile_bytes / 2 / 4e6 : 0.0);
+  }
+};
 // `room`: bytes of workspace.
-AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, size_t room) {
+AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, int32_t window, size_t room) {
   const long long group = n_heads / c->n_kv_heads, covered = (long long)b->table_width * c->page_size;
-  const long long longest = b->max_kv_len > 0 && b->max_kv_len < covered ? b->max_kv_len : covered;
   const long long rows = b->max_q_len > 0 ? b->max_q_len : (b->n_tokens + b->n_reqs - 1LL) / b->n_reqs;
-  const int columns = columns_of(b, c->n_kv_heads, group, rows);
-  const long long all = attention_tiles(b->n_tokens, (int)group, b->n_reqs, columns);
-  const long long busiest = b->n_reqs * ((rows * group + columns - 1) / columns);
-  const long long groups = (all < busiest ? all : busiest) * c->n_kv_heads;
-  const long long steps = (longest + kStepPositions - 1) / kStepPositions;
-  long long slices = ((long long)kGroupsPerUnit * compute_units() + groups - 1) / groups;
-  const long long worth = (steps + kSliceSteps - 1) / kSliceSteps;
-  if (slices > worth) slices = worth;
-  const size_t fit = room / slice_bytes(c, b, n_heads);
-  if (slices > (long long)fit) slices = (long long)fit;
-  if (slices < 2) slices = 1;
-  if (slices > 4096) slices = 4096;
-  const long long per = (steps + slices - 1) / slices;
-  return {columns, (int)slices, (int)(per > 0 ? per : 1), all * c->n_kv_heads * slices};
+  long long longest = b->max_kv_len > 0 && b->max_kv_len < covered ? b->max_kv_len : covered;
+  if (window > 0 && longest > window + rows) longest = window + rows;
+  const long long steps = longest > 0 ? (longest + kStepPositions - 1) / kStepPositions : 1;
+  const long long fit = (long long)(room / slice_bytes(c, b, n_heads)), most = fit < 1 ? 1 : fit < kMostSlices ? fit : kMostSlices;
+  Estimate e = {};
+  // Prompts next to single tokens are taken for new ones, shorter than the longest context, unless that is much longer than a prompt (a part of a long one
+  // may then stand at its end, and slices that nobody needs cost less than one workgroup that goes through all of it).
+  const bool new_prompts = rows * group > kFewColumns && b->n_tokens < rows * b->n_reqs / 2 && longest <= 4 * rows;
+  e.steps = new_prompts ? (double)((rows + kStepPositions - 1) / kStepPositions) : (double)steps;
+  e.mean_steps = (double)steps - (double)(rows < longest ? rows : longest) / (2 * kStepPositions);
+  e.rows = b->n_tokens;
+  e.heads = n_heads;
+  e.tile_bytes = tile_bytes(c->head_dim);
+  e.units = compute_units();
+  AttentionPlan p = {};
+  double best = 0;
+  static const int kSlices[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
+  static const int kColumns[] = {kFewColumns, kSomeColumns, kManyColumns};
+  for (const int columns : kColumns) {
+    if ((columns == kFewColumns) != (rows * group <= kFewColumns)) continue;
+    // tiles of requests that all have the most rows, or of the whole batch if that is less
+    const long long all = columns == kFewColumns ? b->n_reqs : attention_tiles(b->n_tokens, (int)group, b->n_reqs, columns);
+    const long long busiest = b->n_reqs * ((rows * group + columns - 1) / columns);
+    const long long groups = (all < busiest ? all : busiest) * c->n_kv_heads;
+    const long long per_wave = columns == kManyColumns ? 32 : 16;
+    auto share_of = [&](long long live) { return live <= per_wave ? 4 : live <= 2 * per_wave ? 2 : 1; };
+    const int share = share_of(rows * group < columns ? rows * group : columns), mean_share = share_of(b->n_tokens * group * c->n_kv_heads / groups);
+    for (const int slices : kSlices) {
+      if (slices > most || (slices > 1 && slices * share > steps)) break;
+      const double us = e.us(columns, (double)groups, share, mean_share, slices);
+      if (p.columns != 0 && us >= best) continue;
+      best = us;
+      p.columns = columns;
+      p.slices = slices;
+      p.slice_steps = (int)((steps + slices - 1) / slices);
+      p.workgroups = all * c->n_kv_heads * slices;
+    }
+  }
+  return p;
 }
 
 }  // namespace
@@ -253,7 +286,7 @@ int sgmv_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t la
   const size_t reqs = 4 * (size_t)b->n_reqs;
   const Span read[] = {{b->q_starts, reqs + 4}, {b->kv_lens, reqs}, {b->tables, reqs * (size_t)b->table_width}, pages_of(c)};
   if (!aligned(lse, 4) || !aligned(b->q_starts, 4) || !aligned(b->kv_lens, 4) || !aligned(b->tables, 4)) return SGMV_ERR_ALIGN;
-  const AttentionPlan plan = plan_attention(c, b, n_heads, workspace == nullptr ? 0 : workspace_bytes);
+  const AttentionPlan plan = plan_attention(c, b, n_heads, window, workspace == nullptr ? 0 : workspace_bytes);
   const size_t partials = plan.slices > 1 ? slice_bytes(c, b, n_heads) * (size_t)plan.slices : 0;
   const Rows outs = rows_of(out, n, values, out_stride), qs = rows_of(q, n, values, q_stride);
   const Span sums = {lse, 4 * (size_t)n * (size_t)n_heads}, scratch = {partials > 0 ? workspace : nullptr, partials};
@@ -281,6 +314,8 @@ int sgmv_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t la
   a.kv_lens = b->kv_lens;
   a.tables = b->tables;
   a.columns = plan.columns;
+  const long long covered = (long long)b->table_width * c->page_size, hint = b->max_kv_len > 0 && b->max_kv_len < covered ? b->max_kv_len : covered;
+  a.classes = 8.0f / (float)(window > 0 && window < hint ? window : hint + 1);
   a.slices = plan.slices;
   a.slice_steps = plan.slice_steps;
   a.sums = static_cast<float*>(workspace);
@@ -291,21 +326,23 @@ int sgmv_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t la
   return err == hipSuccess ? SGMV_OK : SGMV_ERR_LAUNCH;
 }
 
-size_t sgmv_attention_workspace_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads) {
+size_t sgmv_attention_workspace_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, int32_t window) {
   bool nothing = false;
-  if (check_attention(c, b, n_heads, nullptr, 0, &nothing) != SGMV_OK || nothing) return 0;
-  const AttentionPlan plan = plan_attention(c, b, n_heads, SIZE_MAX / 2);
+  if (window < 0 || check_attention(c, b, n_heads, nullptr, 0, &nothing) != SGMV_OK || nothing) return 0;
+  const AttentionPlan plan = plan_attention(c, b, n_heads, window, SIZE_MAX / 2);
   return plan.slices > 1 ? slice_bytes(c, b, n_heads) * (size_t)plan.slices : 0;
 }
 
-int sgmv_plan_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, const void* workspace, size_t workspace_bytes,
-                           sgmv_plan* plan) {
+int sgmv_plan_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, int32_t window, const void* workspace,
+                           size_t workspace_bytes, sgmv_plan* plan) {
   if (plan == nullptr) return SGMV_ERR_NULL;
   *plan = sgmv_plan{};
   bool nothing = false;
   const int rc = check_attention(c, b, n_heads, workspace, workspace_bytes, &nothing);
-  if (rc != SGMV_OK || nothing) return rc;
-  const AttentionPlan p = plan_attention(c, b, n_heads, workspace == nullptr ? 0 : workspace_bytes);
+  if (rc != SGMV_OK) return rc;
+  if (window < 0) return SGMV_ERR_SHAPE;
+  if (nothing) return rc;
+  const AttentionPlan p = plan_attention(c, b, n_heads, window, workspace == nullptr ? 0 : workspace_bytes);
   plan->kernel = p.columns == kFewColumns ? SGMV_KERNEL_ATTENTION_FEW : SGMV_KERNEL_ATTENTION_MANY;
   plan->launches = p.slices > 1 ? 2 : 1;
   plan->slices = p.slices;

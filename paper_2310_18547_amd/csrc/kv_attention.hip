@@ -75,6 +75,38 @@ __device__ __forceinline__ bool tile_of_batch(const AttentionArgs& a, int column
   return true;
 }
 
+// The n-th of the requests, long ones first: sixty-four of them at a time in eight classes of their lengths next to the longest that the
+// caller expects.  The last workgroups of a launch are then short ones, and no long one is left running alone behind the others.
+__device__ __forceinline__ int request_by_length(const AttentionArgs& a, int n) {
+  const int lane = threadIdx.x & 63, first = n & ~63, i = first + lane;
+  int of = -1;
+  if (i < a.n_reqs) {
+    const int len = a.kv_lens[i];
+    of = min((int)((float)(a.window > 0 ? min(len, a.window) : len) * a.classes), 7);
+    of = max(of, 0);
+  }
+  int rank = n - first;
+  unsigned long long same = 0;
+  for (int k = 7; k >= 0; --k) {
+    same = __ballot(of == k);
+    const int count = __popcll(same);
+    if (rank < count) break;
+    rank -= count;
+  }
+  const bool mine = (same >> lane & 1) && (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0)) == rank;
+  return first + __builtin_ctzll(__ballot(mine) | 1ULL << 63);
+}
+// That request's columns from 0 on; false where it has none.
+__device__ __forceinline__ bool whole_request(const AttentionArgs& a, int request, Tile& t) {
+  t.request = request;
+  t.first_row = clamp_int(a.q_starts[request], 0, a.n_tokens);
+  t.rows = clamp_int(a.q_starts[request + 1], t.first_row, a.n_tokens) - t.first_row;
+  t.columns = t.rows * a.group;
+  t.first_column = 0;
+  t.kv_len = clamp_int(a.kv_lens[request], 0, a.table_width << a.at.page_shift);
+  return t.rows > 0;
+}
+
 // Positions [low, high) that a row of the request sees.
 struct Span {
   int low, high;
@@ -168,6 +200,15 @@ __device__ __forceinline__ float of_lane(float v) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x150 + I, 0xF, 0xF, true));
 }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// Two values as binary16, to the nearest even.
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
+}
+
 // q of one column as the second operand of S^T = K q^T, times a power of two that brings its largest value to between 2^13 and 2^14.
 template <int D>
 struct Query {
@@ -178,50 +219,46 @@ struct Query {
 template <class DT, int D>
 __device__ __forceinline__ void load_query(const AttentionArgs& a, const uint16_t* q, bool live, int lane, Query<D>& out) {
   const int g = lane >> 4;
-  float x[D / 4];
+  uint4 x[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) x[c] = live ? load128(q + g * (D / 4) + c * 8) : make_uint4(0, 0, 0, 0);
+  // the largest magnitude, as a pattern
+  u16x2 most = {0, 0};
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
-    float part[8] = {};
-    if (live) unpack8<DT>(load128(q + g * (D / 4) + c * 8), part);
+    const uint32_t words[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[c * 8 + i] = part[i];
+    for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, words[i] & 0x7FFF7FFFu));
   }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < D / 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+  uint32_t top = max((uint32_t)most.x, (uint32_t)most.y);
   top = max(top, (uint32_t)__shfl_xor((int)top, 16));
   top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-  // 2^up times a value of exponent 13 - up; not finite, or 2^100 and more: the column is NaN
-  const bool fits = top < 0x71800000u;
-  const int up = fits ? 13 - ((int)(top >> 23) - 127) : 0;
+  const float largest = decode1<DT>((uint16_t)top);
+  // not finite, or 2^100 and more: the column is NaN, whatever its operands
+  const bool fits = largest < 0x1p100f;
+  const int up = 13 - ((int)(__float_as_uint(largest) >> 23) - 127);
   float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < D / 4; ++i) {
-    x[i] = fits ? ldexpf(x[i], up) : 0.0f;
-    sum += x[i];
+  for (int c = 0; c < D / 32; ++c) {
+    float v[8];
+    unpack8<DT>(x[c], v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = ldexpf(v[i], up);
+      sum += v[i];
+    }
+    out.parts[c] = make_uint4(pack_half(v[0], v[4]), pack_half(v[1], v[5]), pack_half(v[2], v[6]), pack_half(v[3], v[7]));
   }
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
   out.sum = sum * 0x1p-20f;
   out.factor = fits ? ldexpf(a.scale * 1.44269504088896341f, 20 - up) : __uint_as_float(0x7FC00000u);
-#pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    const float* v = x + c * 8;
-    out.parts[c] = make_uint4(pack2<F16>(v[0], v[4]), pack2<F16>(v[1], v[5]), pack2<F16>(v[2], v[6]), pack2<F16>(v[3], v[7]));
-  }
 }
 
 // First of the values whose row 4 g + i of output tile j a lane receives: value_of + j.
 template <int D>
 __device__ __forceinline__ int value_of(int row) {
   return D == 128 ? 8 * row : 8 * (row & 7) + 4 * (row >> 3);
-}
-
-// Two values as binary16, to the nearest even.
-__device__ __forceinline__ uint32_t pack_half(float a, float b) {
-  typedef float f2 __attribute__((ext_vector_type(2)));
-  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2));
 }
 
 // A wave's columns: NT tiles of sixteen, a column's softmax in the four lanes that hold it (a quarter of the positions' sums each).
@@ -415,7 +452,11 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
   auto steps_before = [&](int step) { return clamp_int((step - begin + stride - 1) >> stride_log2, 0, count); };
   const int head = steps_before((c.all.low + kStepPositions - 1) / kStepPositions), tail = max(steps_before(c.all.high / kStepPositions), head);
   const int ends = head + count - tail;
-  auto step_at = [&](int n) { return begin + ((n < head ? n : n < ends ? n - head + tail : n - ends + head) << stride_log2); };
+  // (behind the last one that one again: what is loaded ahead of nothing comes from a cache)
+  auto step_at = [&](int n) {
+    n = min(n, count - 1);
+    return begin + ((n < head ? n : n < ends ? n - head + tail : n - ends + head) << stride_log2);
+  };
   Held<D> held;
   // pages are looked up two steps ahead of their use: a scalar load's wait is for all of them
   Looked pages = look_up(a, p, step_at(1));
@@ -456,12 +497,22 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
   }
 }
 
-// A wave's columns, from column `first` of the request on, and the steps [from, from + steps) of this slice that they look at.
+// Steps [begin, end) of a slice.  `whole`: the first slice has all of the tile's, so its result is the rows', and not a part to be joined.
 struct Steps {
   int begin, end;
+  bool whole;
 };
+__device__ __forceinline__ Steps steps_of_slice(const AttentionArgs& a, const Tile& t, int columns, int slice) {
+  const Span lowest = seen_by(a, t, t.first_column / a.group), highest = seen_by(a, t, (t.first_column + columns - 1) / a.group);
+  const int from = lowest.low / kStepPositions;
+  const int steps = highest.high > lowest.low ? (highest.high + kStepPositions - 1) / kStepPositions - from : 0;
+  const int per = max(a.slice_steps, (steps + a.slices - 1) / a.slices);
+  return {from + min(steps, slice * per), from + min(steps, (slice + 1) * per), steps <= per};
+}
+
+// A wave's columns, from column `first` of the request on, and those of the slice's steps that they look at.
 template <class DT, int D, int NT>
-__device__ __forceinline__ Steps load_columns(const AttentionArgs& a, const Tile& t, int first, int head, int slice, int lane, Columns<D, NT>& c, Pages& p) {
+__device__ __forceinline__ Steps load_columns(const AttentionArgs& a, const Tile& t, int first, int head, const Steps& slice, int lane, Columns<D, NT>& c, Pages& p) {
   start_columns<D, NT>(c, lane);
   const int last_column = min(first + 16 * NT, t.columns) - 1;
   const Span lowest = seen_by(a, t, first / a.group), highest = seen_by(a, t, last_column / a.group);
@@ -478,10 +529,8 @@ __device__ __forceinline__ Steps load_columns(const AttentionArgs& a, const Tile
   p.table = (const __attribute__((address_space(4))) int32_t*)(a.tables + (size_t)t.request * a.table_width);
   p.head = a.at.layer + (size_t)head * ((1u << a.at.page_shift) / kTilePositions) * tile_bytes(D);
   p.last_tile = (c.some.high - 1) / kTilePositions;
-  const int from = c.some.low / kStepPositions;
-  const int steps = c.some.high > c.some.low ? (c.some.high + kStepPositions - 1) / kStepPositions - from : 0;
-  const int per = max(a.slice_steps, (steps + a.slices - 1) / a.slices);
-  return {from + min(steps, slice * per), from + min(steps, (slice + 1) * per)};
+  const int end = c.some.high > c.some.low ? (c.some.high + kStepPositions - 1) / kStepPositions : 0;
+  return {max(slice.begin, c.some.low / kStepPositions), min(slice.end, end), slice.whole};
 }
 
 // Sums of a column over its four lanes.
@@ -494,15 +543,20 @@ __device__ __forceinline__ float log_sum(float base, float sum) {
   return sum == 0.0f ? -__uint_as_float(0x7F800000u) : (base + log2f(sum)) * 0.693147180559945309f;
 }
 
-// Output of a column's values from `value` on: v unnormalised.
+// What the sum of a row's first slice is where that slice has been written as the row's result.
+constexpr float kWritten = -1.0f;
+
+// Values of a column from `value` on, unnormalised, into the result (whole) or into the slice's part.
 template <class DT, int D, int N>
-__device__ __forceinline__ void put_values(const AttentionArgs& a, long long row, int q_head, int slice, int value, const float (&v)[N], float sum, float inverse) {
-  if (a.slices > 1) {
+__device__ __forceinline__ void put_values(const AttentionArgs& a, bool whole, long long row, int q_head, int slice, int value, const float (&v)[N], float sum) {
+  if (!whole) {
+    if (sum == 0.0f) return;  // the join passes such parts by
     const size_t part = ((size_t)row * a.n_heads + q_head) * a.slices + slice;
 #pragma unroll
     for (int k = 0; k < N; k += 4) *reinterpret_cast<float4*>(a.sums + part * D + value + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
     return;
   }
+  const float inverse = 1.0f / sum;
   uint2* to = reinterpret_cast<uint2*>(a.out + row * a.out_stride + q_head * D + value);
 #pragma unroll
   for (int k = 0; k < N; k += 4) {
@@ -512,12 +566,10 @@ __device__ __forceinline__ void put_values(const AttentionArgs& a, long long row
     to[k / 4] = make_uint2(pack2<DT>(w[0], w[1]), pack2<DT>(w[2], w[3]));
   }
 }
-__device__ __forceinline__ void put_sum(const AttentionArgs& a, long long row, int q_head, int slice, float base, float sum) {
+__device__ __forceinline__ void put_sum(const AttentionArgs& a, bool whole, long long row, int q_head, int slice, float base, float sum) {
   const size_t item = (size_t)row * a.n_heads + q_head;
-  if (a.slices > 1)
-    a.tops[item * a.slices + slice] = make_float2(base, sum);
-  else if (a.lse != nullptr)
-    a.lse[item] = log_sum(base, sum);
+  if (whole && a.lse != nullptr) a.lse[item] = log_sum(base, sum);
+  if (a.slices > 1) a.tops[item * a.slices + slice] = make_float2(base, whole ? kWritten : sum);
 }
 
 // What the waves of a workgroup that share columns hand to one another.
@@ -534,15 +586,17 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
   const int groups_log2 = columns <= PER ? 0 : columns <= 2 * PER ? 1 : 2, group = wave & ((1 << groups_log2) - 1);
   const int first = t.first_column + group * PER;
+  const Steps of_slice = steps_of_slice(a, t, columns, slice);
+  if (of_slice.whole && slice > 0) return;
   Columns<D, NT> c;
   if (first < t.columns) {
     Pages p;
-    const Steps steps = load_columns<DT, D, NT>(a, t, first, head, slice, lane, c, p);
+    const Steps steps = load_columns<DT, D, NT>(a, t, first, head, of_slice, lane, c, p);
     attend_steps<DT, D, NT>(a, p, steps.begin + (wave >> groups_log2), steps.end, 2 - groups_log2, lane, c);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float sum = of_column(c.sum[n]), minima = of_column(c.minima[n]);
-      const float base = c.top[n] == kLowest ? kLowest : c.base[n], inverse = 1.0f / sum;
+      const float base = c.top[n] == kLowest ? kLowest : c.base[n];
       const int column = first + n * 16 + i;
       if (column >= t.columns) continue;
       const int row = column / a.group, q_head = head * a.group + column - row * a.group;
@@ -558,14 +612,14 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
         } else {
 #pragma unroll
           for (int j = 0; j < D / 16; ++j) v[j] += minima;
-          put_values<DT, D>(a, t.first_row + row, q_head, slice, value, v, sum, inverse);
+          put_values<DT, D>(a, of_slice.whole, t.first_row + row, q_head, slice, value, v, sum);
         }
       }
       if (g != 0) continue;
       if (groups_log2 < 2)
         shared.stats[wave][n * 16 + i] = make_float4(base, sum, minima, 0.0f);
       else
-        put_sum(a, t.first_row + row, q_head, slice, base, sum);
+        put_sum(a, of_slice.whole, t.first_row + row, q_head, slice, base, sum);
     }
   }
   if (groups_log2 == 2) return;
@@ -589,59 +643,77 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) v[k] += minima;
     const int column = t.first_column + of_tile, row = column / a.group, q_head = head * a.group + column - row * a.group;
-    put_values<DT, D>(a, t.first_row + row, q_head, slice, part * (D / 16), v, sum, 1.0f / sum);
-    if (part == 0) put_sum(a, t.first_row + row, q_head, slice, base, sum);
+    put_values<DT, D>(a, of_slice.whole, t.first_row + row, q_head, slice, part * (D / 16), v, sum);
+    if (part == 0) put_sum(a, of_slice.whole, t.first_row + row, q_head, slice, base, sum);
   }
 }
 
-// 2^COLUMNS_LOG2 columns of one cache head, 16 (few) or 64 NT of them.  grid = (cache heads x tiles, slices); the last tiles, which see most,
-// first.
-template <class DT, int D, int NT, int COLUMNS_LOG2>
-__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_kernel(AttentionArgs a, int first_tile, int tiles) {
+// 64 NT columns of one cache head.  grid = (cache heads x tiles, slices); the last tiles, which see most, first.
+template <class DT, int D, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_many_kernel(AttentionArgs a, int first_tile, int tiles) {
   __shared__ Shared<D, NT> shared;
   const int head = blockIdx.x % a.at.n_kv_heads, tile = first_tile + tiles - 1 - (int)(blockIdx.x / a.at.n_kv_heads), slice = blockIdx.y;
   Tile t;
-  if (!tile_of_batch(a, COLUMNS_LOG2, tile, t)) return;
-  const int columns = min(t.columns - t.first_column, 1 << COLUMNS_LOG2);
+  if (!tile_of_batch(a, NT == 1 ? 6 : 7, tile, t)) return;
+  const int columns = min(t.columns - t.first_column, 64 * NT);
   if (NT > 1 && columns <= 16)
     attend_tile<DT, D, 1>(a, t, columns, head, slice, reinterpret_cast<Shared<D, 1>&>(shared));
   else
     attend_tile<DT, D, NT>(a, t, columns, head, slice, shared);
 }
 
-// Joins the slices of a row's head: D / 4 threads take four values each, the others of the workgroup other slices.  grid = rows x heads.
+// Requests of up to sixteen columns (more than the hint said: sixteen after sixteen).  grid = (cache heads x requests, slices).
 template <class DT, int D>
+__global__ __launch_bounds__(256, 3) void attention_few_kernel(AttentionArgs a, int first_request) {
+  __shared__ Shared<D, 1> shared;
+  const int head = blockIdx.x % a.at.n_kv_heads, request = request_by_length(a, first_request + (int)(blockIdx.x / a.at.n_kv_heads)), slice = blockIdx.y;
+  Tile t;
+  if (!whole_request(a, request, t)) return;
+  for (; t.first_column < t.columns; t.first_column += kFewColumns) {
+    attend_tile<DT, D, 1>(a, t, min(t.columns - t.first_column, kFewColumns), head, slice, shared);
+    __syncthreads();
+  }
+}
+
+// Joins the slices of rows' heads that are in parts: D / 4 threads take four values each, GROUPS such sets of threads the slices of one head in turn
+// (few rows, many slices) or, with one, a head each.  grid = rows x heads / (256 / (GROUPS D / 4)).
+template <class DT, int D, int GROUPS>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, long long first) {
-  constexpr int THREADS = D / 4, GROUPS = 256 / THREADS;
+  constexpr int THREADS = D / 4, ITEMS = 256 / (THREADS * GROUPS);
   __shared__ float4 parts[GROUPS][THREADS];
   __shared__ float sums[GROUPS];
-  const long long item = first + blockIdx.x;
-  const int lane = threadIdx.x & 63, part = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
+  const int part = threadIdx.x % THREADS, group = threadIdx.x / THREADS % GROUPS;
+  const long long item = first + (long long)blockIdx.x * ITEMS + threadIdx.x / (THREADS * GROUPS);
+  if (item >= (long long)a.n_tokens * a.n_heads) return;
   const int row = (int)(item / a.n_heads), head = (int)(item - (long long)row * a.n_heads);
   if (row < a.q_starts[0] || row >= a.q_starts[a.n_reqs]) return;
   const float2* tops = a.tops + item * a.slices;
+  if (tops[0].y == kWritten) return;
   float top = kLowest;
-  for (int z = lane; z < a.slices; z += 64) top = fmaxf(top, tops[z].x);
+  for (int z = part; z < a.slices; z += THREADS) top = fmaxf(top, tops[z].x);
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+  for (int m = 1; m < THREADS; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float sum = 0.0f;
 #pragma unroll 4
   for (int z = group; z < a.slices; z += GROUPS) {
     const float2 of = tops[z];
+    if (of.y == 0.0f) continue;  // a slice that sees nothing: no values are there
     const float4 x = *reinterpret_cast<const float4*>(a.sums + (item * a.slices + z) * D + part * 4);
     const float w = __builtin_amdgcn_exp2f(of.x - top);
     sum = fmaf(w, of.y, sum);
     v.x = fmaf(w, x.x, v.x), v.y = fmaf(w, x.y, v.y), v.z = fmaf(w, x.z, v.z), v.w = fmaf(w, x.w, v.w);
   }
-  parts[group][part] = v;
-  if (part == 0) sums[group] = sum;
-  __syncthreads();
-  if (group != 0) return;
-  for (int k = 1; k < GROUPS; ++k) {
-    const float4 x = parts[k][part];
-    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-    sum += sums[k];
+  if (GROUPS > 1) {
+    parts[group][part] = v;
+    if (part == 0) sums[group] = sum;
+    __syncthreads();
+    if (group != 0) return;
+    for (int k = 1; k < GROUPS; ++k) {
+      const float4 x = parts[k][part];
+      v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+      sum += sums[k];
+    }
   }
   const float inverse = 1.0f / sum;
   const bool none = sum == 0.0f;
@@ -652,9 +724,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, lo
 
 // Launches over ranges of tiles, fewer than 2^31 threads each.
 template <class F>
-hipError_t by_tiles(const AttentionArgs& a, int columns, F launch) {
-  const long long tiles = attention_tiles(a.n_tokens, a.group, a.n_reqs, columns);
-  const long long share = (1LL << 30) / 256 / a.slices / a.at.n_kv_heads, most = share > 0 ? share : 1;
+hipError_t by_tiles(const AttentionArgs& a, F launch) {
+  const long long tiles = a.columns == kFewColumns ? a.n_reqs : attention_tiles(a.n_tokens, a.group, a.n_reqs, a.columns);
+  // whole sixty-fours of requests
+  const long long share = (1LL << 30) / 256 / a.slices / a.at.n_kv_heads & ~63LL, most = share > 0 ? share : 64;
   for (long long first = 0; first < tiles; first += most) {
     const long long n = tiles - first < most ? tiles - first : most;
     launch(dim3((unsigned)(n * a.at.n_kv_heads), (unsigned)a.slices), (int)first, (int)n);
@@ -666,22 +739,28 @@ hipError_t by_tiles(const AttentionArgs& a, int columns, F launch) {
 
 template <class DT, int D>
 hipError_t columns_typed(const AttentionArgs& a, hipStream_t st) {
-  return by_tiles(a, a.columns, [&](dim3 grid, int first, int n) {
+  return by_tiles(a, [&](dim3 grid, int first, int n) {
     if (a.columns == kFewColumns)
-      attention_kernel<DT, D, 1, 4><<<grid, 256, 0, st>>>(a, first, n);
+      attention_few_kernel<DT, D><<<grid, 256, 0, st>>>(a, first);
     else if (a.columns == kSomeColumns)
-      attention_kernel<DT, D, 1, 6><<<grid, 256, 0, st>>>(a, first, n);
+      attention_many_kernel<DT, D, 1><<<grid, 256, 0, st>>>(a, first, n);
     else
-      attention_kernel<DT, D, 2, 7><<<grid, 256, 0, st>>>(a, first, n);
+      attention_many_kernel<DT, D, 2><<<grid, 256, 0, st>>>(a, first, n);
   });
 }
 
 template <class DT, int D>
 hipError_t join_typed(const AttentionArgs& a, hipStream_t st) {
+  constexpr int kAll = 256 / (D / 4);
+  // a workgroup to a head while these are few; with many, one after the other has enough to load
+  const bool few = (long long)a.n_tokens * a.n_heads <= 4096;
   const long long items = (long long)a.n_tokens * a.n_heads, most = 1LL << 22;
   for (long long first = 0; first < items; first += most) {
     const long long n = items - first < most ? items - first : most;
-    attention_join_kernel<DT, D><<<(unsigned)n, 256, 0, st>>>(a, first);
+    if (few)
+      attention_join_kernel<DT, D, kAll><<<(unsigned)n, 256, 0, st>>>(a, first);
+    else
+      attention_join_kernel<DT, D, 1><<<(unsigned)((n + kAll - 1) / kAll), 256, 0, st>>>(a, first);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }

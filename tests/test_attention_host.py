@@ -164,14 +164,14 @@ def test_plans_and_workspaces():
     one = batch(n_reqs=1, n_tokens=1, table_width=8192, max_q_len=1, max_kv_len=131072)
     for b in (many, one):
         need = sg.sgmv_attention_workspace_bytes(c, b, 32)
-        plan = sg.sgmv_plan_attention_q4(c, b, 32, AT["workspace"], need)
+        plan = sg.sgmv_plan_attention_q4(c, b, 32, 0, AT["workspace"], need)
         assert (plan.slices > 1) == (need > 0) and plan.launches == (2 if need else 1)
         assert need == b.n_tokens * 32 * (4 * 128 + 8) * plan.slices * (plan.slices > 1)
         without = sg.sgmv_plan_attention_q4(c, b, 32)
         assert without.slices == 1 and without.launches == 1
-        half = sg.sgmv_plan_attention_q4(c, b, 32, AT["workspace"], need // 2)
+        half = sg.sgmv_plan_attention_q4(c, b, 32, 0, AT["workspace"], need // 2)
         assert half.slices <= max(1, plan.slices // 2)
-    assert sg.sgmv_plan_attention_q4(c, one, 32, AT["workspace"], 1 << 30).slices > 8
+    assert sg.sgmv_plan_attention_q4(c, one, 32, 0, AT["workspace"], 1 << 30).slices > 8
     assert sg.sgmv_attention_workspace_bytes(c, batch(n_reqs=1, n_tokens=1, table_width=1), 32) == 0
     assert sg.sgmv_attention_workspace_bytes(c, batch(n_reqs=0), 32) == 0 and sg.sgmv_attention_workspace_bytes(c, batch(), 33) == 0
     rc, _ = sg.sgmv_plan_attention_q4(c, batch(), 33, check=False)
