@@ -18,12 +18,14 @@ library's kernels, issued three ways:
 
 ``--backbone q8`` holds the layer's own weights in 8-bit integers instead (``layer.Q8Layer``): the projections are
 this library's kernels too, and a step is the whole layer but attention -- norms, 8-bit rows, gated activation and
-the seven projections -- without (``backbone``) and with the add-ons (``lora_multi``).
+the seven projections -- without (``backbone``) and with the add-ons (``lora_multi``).  ``--context N`` adds attention
+(``layer.KvCacheQ4``): every request has N positions in a paged 4-bit cache, to which a step's rows are appended
+(heads of 128, rotary positions), and ``attention`` is the time of that part.
 
 Consecutive steps cycle over ``--layers`` sets of backbone and adapter weights so that nothing
 is served from the on-die caches.  Everything is synthetic (random weights, as in the paper's
 microbenchmarks).  Prints ONE JSON line.  This follows the paper's transformer-layer
-benchmark in spirit only: no attention kernel, one GPU.
+benchmark in spirit only: attention only with ``--context``, one GPU.
 """
 from __future__ import annotations
 
@@ -48,6 +50,7 @@ def main():
                     help="adapter popularity over the --batch decode rows (the operator microbenchmark's mixes): "
                          "rows that share an adapter form one segment")
     ap.add_argument("--backbone", choices=["f16", "q8"], default="f16", help="the layer's own weights: 16-bit floats or 8-bit integers")
+    ap.add_argument("--context", type=int, default=-1, help="with --backbone q8: positions of every request in the 4-bit cache before the step")
     ap.add_argument("--rank", type=int, default=16)
     ap.add_argument("--layers", type=int, default=4, help="weight sets cycled through")
     ap.add_argument("--steps", type=int, default=200)
@@ -59,6 +62,7 @@ def main():
     from paper_2310_18547_amd import binding as B
 
     assert torch.cuda.is_available(), "bench_layer.py needs a GPU"
+    assert args.context < 0 or args.backbone == "q8", "--context goes with --backbone q8"
     dev = torch.device("cuda:0")
     h, ffn = MODELS[args.model]
     n_req, r, L = args.batch, args.rank, args.layers
@@ -187,10 +191,33 @@ def main():
             layer.qkv(None, residual, i % L, stream=sh)
             layer.finish(attention, residual, i % L, stream=sh)
 
+        cache = None
+        if args.context >= 0:
+            from paper_2310_18547_amd.layer import KvCacheQ4
+            places, page = args.batch, 16
+            longest = args.context + args.seq
+            cache = KvCacheQ4(B.F16, 128, h // 128, h // 128, L, page, places * -(-longest // page), places, T, longest, max_q_len=args.seq,
+                              max_kv_len=longest)
+            left = args.context
+            while left:  # the contexts, as many positions of every request at a time as the step has rows
+                now = min(left, args.seq)
+                cache.step(torch.full((places,), now, dtype=torch.int32, device=dev))
+                kv = rnd(T, h), rnd(T, h)
+                for l in range(L):
+                    cache.append(l, attention, *kv)
+                left -= now
+            cache.step(torch.full((places,), args.seq, dtype=torch.int32, device=dev))
+            assert cache.check() == 0
+
+            def step_q8(i):
+                layer.run(None, residual, i % L, cache, stream=sh)
+
         layer.add_ons = False
         res = {"backbone_us": timeit(step_q8)}
         layer.add_ons = True
         res["lora_multi_us"] = timeit(step_q8)
+        if cache is not None:
+            res["attention_us"] = timeit(lambda i: cache.run(i % L, layer.y["q"], layer.y["k"], layer.y["v"], stream=sh))
         assert layer.check(sh) == 0
     else:
         res = {"backbone_us": timeit(step_backbone), "lora_single_us": timeit(step_single),
@@ -200,7 +227,7 @@ def main():
     lora = sum((i * r + r * o) for i, o in shapes.values()) * 2 * n_req
     out = {"benchmark": "decoder-layer dense projections + LoRA add-ons", "backbone": args.backbone,
            "model": args.model, "h": h, "ffn": ffn, "batch": args.batch, "seq": args.seq, "mix": args.mix,
-           "adapters": n_req, "tokens": T, "rank": r,
+           "adapters": n_req, "tokens": T, "rank": r, **({"context": args.context, "kv_cache": "4 bits"} if args.context >= 0 else {}),
            "layers_cycled": L,
            "steps": args.steps, "dtype": "f16", "data": "synthetic", "n_gpus": 1,
            "backbone_weight_bytes_per_step": weights, "adapter_weight_bytes_per_step": lora,

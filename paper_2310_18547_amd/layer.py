@@ -9,12 +9,13 @@ one ``sgmv_add_lora_multi`` call each, o and down are single ``sgmv_add_lora`` c
 calls share one workspace and must be enqueued on one stream.
 
 ``Q8Layer`` is a layer whose own weights are held in 8-bit integers: besides the add-ons it
-issues the norms, the dense projections and the gated activation that they stand between,
-everything of the layer but attention.
+issues the norms, the dense projections and the gated activation that they stand between.
+``KvCacheQ4`` is what attention needs: a paged cache in 4 bits, its block tables and the calls
+between the q / k / v and the o projections.  ``Q8Layer.run`` strings the two together.
 """
 from __future__ import annotations
 
-from typing import Dict, Sequence
+from typing import Dict, Optional, Sequence
 
 import torch
 
@@ -93,6 +94,99 @@ def _require(t, kind, rows: int, width: int, device, what: str, exactly: bool = 
             return
         got = f"{tuple(t.shape)} of {t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}"
     raise ValueError(f"{what}: {rows} contiguous rows of {width} {kind} on {device}, not {got}")
+
+
+class KvCacheQ4:
+    """The paged cache of a batch of ``n_reqs`` places for requests, ``n_tokens`` rows a step, and attention over it.
+
+    A request keeps its place from its prompt to its end, and its rows of a step lie behind those of the places before it.
+    ``step`` tells the cache what every place brings; then every layer calls ``run`` (or ``append`` and ``attend``).  Places
+    that bring nothing have no rows.  All of it stays on the device: a captured step, replayed, goes on by itself.
+
+    ``rope_dim`` values of a head are rotated by their position (``None``: all, 0: none), with base ``rope_base`` and pairs
+    ``(i, i + rope_dim / 2)``, or ``(2 i, 2 i + 1)`` with ``adjacent``.  ``max_q_len`` and ``max_kv_len`` are hints for the kernels'
+    shapes (:meth:`hint`).  One call at a time, on one stream.
+    """
+
+    def __init__(self, dtype: int, head_dim: int, n_heads: int, n_kv_heads: int, num_layers: int, page_size: int, n_pages: int, n_reqs: int,
+                 n_tokens: int, max_len: int, rope_dim: Optional[int] = None, rope_base: float = 10000.0, adjacent: bool = False,
+                 scale: Optional[float] = None, window: int = 0, max_q_len: int = 0, max_kv_len: int = 0, device="cuda:0"):
+        self.dtype, self.head_dim, self.n_heads, self.n_kv_heads, self.n_tokens, self.n_reqs = dtype, head_dim, n_heads, n_kv_heads, n_tokens, n_reqs
+        self.kind = kind = torch.float16 if dtype == B.F16 else torch.bfloat16
+        self.scale, self.window = head_dim ** -0.5 if scale is None else scale, window
+        self.width = -(-max_len // page_size)
+        page_bytes = B.sgmv_kv_page_bytes(B.make_kv_cache(dtype, head_dim, n_kv_heads, num_layers, page_size, n_pages))
+        if page_bytes == 0:
+            raise ValueError(f"no cache of {n_pages} pages of {page_size} positions, {num_layers} layers of {n_kv_heads} heads of {head_dim}")
+        if n_heads <= 0 or n_heads % n_kv_heads or n_reqs <= 0 or n_tokens <= 0 or max_len <= 0:
+            raise ValueError(f"{n_heads} heads over {n_kv_heads}, {n_reqs} requests, {n_tokens} rows, {max_len} positions")
+
+        def ints(*shape, value=0):
+            return torch.full(shape, value, dtype=torch.int32, device=device)
+
+        # unwritten positions are never looked at, so nothing has to be cleared
+        self.pages = torch.empty(n_pages, page_bytes, dtype=torch.uint8, device=device)
+        self.tables, self.lens, self.q_starts = ints(n_reqs, self.width, value=-1), ints(n_reqs), ints(n_reqs + 1)
+        self.slots, self.positions = ints(n_tokens, value=-1), ints(n_tokens, value=-1)
+        self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
+        self.free_count, self.status = ints(1, value=n_pages), ints(2)
+        self.cache = B.make_kv_cache(dtype, head_dim, n_kv_heads, num_layers, page_size, n_pages, self.pages)
+        self.batch = B.make_kv_batch(n_reqs, n_tokens, self.width, self.q_starts, self.lens, self.tables, self.slots, self.positions)
+        rope_dim = head_dim if rope_dim is None else rope_dim
+        self.rope = None
+        if rope_dim:
+            # angles in 64 bits: far positions have many turns behind them
+            angles = torch.arange(max_len, dtype=torch.float64)[:, None] * rope_base ** (-torch.arange(rope_dim // 2, dtype=torch.float64) / (rope_dim // 2))
+            self.rope_table = torch.cat((angles.cos(), angles.sin()), 1).to(torch.float32).to(device)
+            self.rope = B.make_rope(self.rope_table, max_len, rope_dim, int(adjacent))
+        self.q = torch.zeros(n_tokens, n_heads * head_dim, dtype=kind, device=device)    # rotated
+        self.out = torch.zeros(n_tokens, n_heads * head_dim, dtype=kind, device=device)
+        self.hint(max_q_len, max_kv_len)
+        self.scratch_bytes = self._scratch_bytes()
+        self.scratch = torch.empty(max(self.scratch_bytes, 256), dtype=torch.uint8, device=device)
+
+    def _scratch_bytes(self) -> int:
+        """Room for the slices of decode steps and of steps as the hints tell, whichever is more."""
+        least = B.make_kv_batch(self.n_reqs, min(self.n_tokens, self.n_reqs), self.width, None, None, None, max_q_len=1,
+                                max_kv_len=self.batch.max_kv_len)
+        return max(B.sgmv_attention_workspace_bytes(self.cache, b, self.n_heads, self.window) for b in (self.batch, least))
+
+    def hint(self, max_q_len: int, max_kv_len: int) -> None:
+        """Most rows that a request brings and most positions that one has, from here on (0: unknown); speed alone depends on them."""
+        self.batch.max_q_len, self.batch.max_kv_len = max_q_len, max_kv_len
+
+    def step(self, new_lens: torch.Tensor, stream=None) -> None:
+        """Pages, slots and positions for what every place brings: ``new_lens`` int32 ``[n_reqs]`` on the device, -1 for a request that is
+        over (its place is free from this step on)."""
+        _require(new_lens[None] if isinstance(new_lens, torch.Tensor) else new_lens, torch.int32, 1, self.n_reqs, self.pages.device, "new_lens")
+        B.sgmv_kv_assign(self.cache, self.batch, new_lens, self.lens, self.free_pages, self.free_count, self.free_count, self.status, stream)
+
+    def append(self, layer_idx: int, q, k, v, stream=None):
+        """k and v of the step's rows into the cache; returns the rows of q that ``attend`` takes (rotated)."""
+        device, width = self.pages.device, self.n_kv_heads * self.head_dim
+        _require(q, self.kind, self.n_tokens, self.n_heads * self.head_dim, device, "q")
+        _require(k, self.kind, self.n_tokens, width, device, "k")
+        _require(v, self.kind, self.n_tokens, width, device, "v")
+        row = self.n_heads * self.head_dim
+        turned = self.rope is not None
+        B.sgmv_kv_append_q4(self.cache, self.batch, layer_idx, self.q if turned else None, q if turned else None, k, v, self.n_heads, row, row, width,
+                            self.rope, stream)
+        return self.q if turned else q
+
+    def attend(self, layer_idx: int, q, stream=None):
+        """Causal attention of the step's rows over their requests' positions; rows of nobody are left as they were."""
+        row = self.n_heads * self.head_dim
+        _require(q, self.kind, self.n_tokens, row, self.pages.device, "q")
+        B.sgmv_attention_q4(self.cache, self.batch, layer_idx, self.out, None, q, self.n_heads, row, row, self.scale, 1, self.window, self.scratch,
+                            self.scratch_bytes, stream)
+        return self.out
+
+    def run(self, layer_idx: int, q, k, v, stream=None):
+        return self.attend(layer_idx, self.append(layer_idx, q, k, v, stream), stream)
+
+    def check(self) -> int:
+        """What was wrong with any step so far (``KV_*``, waits for the device)."""
+        return int(self.status[1])
 
 
 class Q8Layer(LoraLayer):
@@ -197,3 +291,10 @@ class Q8Layer(LoraLayer):
                            stream)
         self.project(("down",), self.q_ffn, self.act, layer_idx, scale, stream)
         return self.y["down"]
+
+    def run(self, x, residual, layer_idx: int, cache: KvCacheQ4, scale: float = 1.0, stream=None):
+        """The whole layer: ``qkv``, attention over ``cache`` (whose ``step`` has been told about these rows), ``finish``."""
+        if (cache.kind, cache.n_tokens, cache.n_heads * cache.head_dim, cache.n_kv_heads * cache.head_dim) != (self.kind, self.n_tokens, self.h, self.h):
+            raise ValueError(f"a cache of {cache.n_tokens} rows of {cache.n_heads} / {cache.n_kv_heads} heads of {cache.head_dim} {cache.kind}, not of "
+                             f"{self.n_tokens} rows of {self.h} {self.kind}")
+        return self.finish(cache.run(layer_idx, *self.qkv(x, residual, layer_idx, scale, stream), stream), residual, layer_idx, scale, stream)

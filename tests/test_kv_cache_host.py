@@ -1,0 +1,76 @@
+"""What KvCacheQ4 and Q8Layer.run take and refuse, without a GPU: their calls are recorded in place of being made."""
+import pytest
+import torch
+
+import paper_2310_18547_amd as sg
+from paper_2310_18547_amd import layer as layer_module
+from paper_2310_18547_amd.layer import KvCacheQ4
+from test_layer_host import FFN, H, KIND, LAYERS, N, _layer, _rows, calls  # noqa: F401
+
+
+@pytest.fixture
+def kv_calls(monkeypatch, calls):  # noqa: F811
+    for name in ("sgmv_kv_assign", "sgmv_kv_append_q4", "sgmv_attention_q4"):
+        monkeypatch.setattr(layer_module.B, name, lambda *a, name=name, **k: calls.append(name) or 0)
+    return calls
+
+
+def _cache(**k):
+    a = dict(dtype=sg.F16, head_dim=64, n_heads=1, n_kv_heads=1, num_layers=LAYERS, page_size=16, n_pages=6, n_reqs=3, n_tokens=N, max_len=50,
+             device="cpu")
+    a.update(k)
+    return KvCacheQ4(**a)
+
+
+def test_cache_and_its_first_state():
+    t = _cache()
+    assert t.width == 4 and t.tables.shape == (3, 4) and int(t.free_count) == 6 and t.free_pages.tolist() == list(range(6))
+    assert t.pages.shape == (6, LAYERS * (16 * 64 + 128)) and t.scale == 64 ** -0.5
+    assert t.rope_table.shape == (50, 64) and t.rope_table[0].tolist() == [1.0] * 32 + [0.0] * 32
+    assert abs(float(t.rope_table[49, 32]) - torch.tensor(49.0, dtype=torch.float64).sin().item()) < 1e-7
+    t.hint(1, 77)
+    assert (t.batch.max_q_len, t.batch.max_kv_len) == (1, 77)
+    assert _cache(rope_dim=0).rope is None and _cache(rope_dim=32).rope_table.shape == (50, 32)
+
+
+@pytest.mark.parametrize("wrong", [dict(head_dim=96), dict(page_size=20), dict(n_pages=0), dict(n_heads=3, n_kv_heads=2), dict(n_reqs=0),
+                                   dict(n_tokens=0), dict(max_len=0), dict(n_heads=0)])
+def test_caches_that_are_refused(wrong):
+    with pytest.raises(ValueError):
+        _cache(**wrong)
+
+
+def test_the_calls_of_a_step(kv_calls):
+    t = _cache()
+    t.step(torch.zeros(3, dtype=torch.int32))
+    q = t.append(0, _rows(), _rows(), _rows())
+    assert q is t.q and t.attend(0, q) is t.out
+    plain = _cache(rope_dim=0)
+    mine = _rows()
+    assert plain.append(1, mine, _rows(), _rows()) is mine
+    assert kv_calls == ["sgmv_kv_assign", "sgmv_kv_append_q4", "sgmv_attention_q4", "sgmv_kv_append_q4"]
+
+
+def test_rows_and_lengths_that_are_not_the_caches(kv_calls):
+    t, good = _cache(), _rows()
+    bad = [_rows(N - 1), _rows(kind=torch.bfloat16), _rows(width=2 * H)[:, :H], _rows(width=H // 2), torch.empty(N, H, dtype=KIND, device="meta"), None]
+    for b in bad:
+        for call in (lambda: t.append(0, b, good, good), lambda: t.append(0, good, b, good), lambda: t.append(0, good, good, b), lambda: t.attend(0, b)):
+            with pytest.raises(ValueError):
+                call()
+    for b in (torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), torch.zeros(6, dtype=torch.int32)[::2], [0, 0, 0]):
+        with pytest.raises(ValueError):
+            t.step(b)
+    assert kv_calls == []
+
+
+def test_a_whole_layer(kv_calls):
+    layer, residual = _layer(), _rows()
+    layer.run(_rows(), residual, 0, _cache())
+    assert kv_calls[:2] == ["sgmv_rms_norm_q8", "sgmv_dense_q8"] and kv_calls.index("sgmv_kv_append_q4") < kv_calls.index("sgmv_attention_q4")
+    assert kv_calls.index("sgmv_attention_q4") < kv_calls.index("sgmv_quantize_q8") and "sgmv_kv_assign" not in kv_calls
+    before = len(kv_calls)
+    for wrong in (dict(n_tokens=N + 1), dict(dtype=sg.BF16), dict(head_dim=128), dict(n_heads=2)):
+        with pytest.raises(ValueError):
+            layer.run(_rows(), residual, 0, _cache(**wrong))
+    assert len(kv_calls) == before and FFN > H
