@@ -73,6 +73,7 @@ struct AttentionArgs {
   int causal, window;
   float scale;
   int columns;               // one of the three
+  int heads_log2;            // kFewColumns: cache heads of a workgroup, one (whose steps its waves share) or 2^2 (a wave each)
   uint16_t* out;
   float* lse;
   const uint16_t* q;
@@ -81,6 +82,7 @@ struct AttentionArgs {
   const int32_t* kv_lens;
   const int32_t* tables;
   float classes;             // classes of lengths for a position (request_by_length)
+  bool ordered;              // tiles by their work (tile_by_work), set at launch
   int slices;                // parts of a tile's positions (workgroups), joined by a second launch where there are several
   int slice_steps;           // steps of a slice at least
   float* sums;               // slices > 1: [n_tokens][n_heads][slices][head_dim] unnormalised, then ...

@@ -75,6 +75,12 @@ __device__ __forceinline__ bool tile_of_batch(const AttentionArgs& a, int column
   return true;
 }
 
+// The lane whose bit is the n-th that is set.
+__device__ __forceinline__ int nth_bit(unsigned long long bits, int n) {
+  const int lane = threadIdx.x & 63, before = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+  return __builtin_ctzll(__ballot((bits >> lane & 1) && before == n) | 1ULL << 63);
+}
+
 // The n-th of the requests, long ones first: sixty-four of them at a time in eight classes of their lengths next to the longest that the
 // caller expects.  The last workgroups of a launch are then short ones, and no long one is left running alone behind the others.
 __device__ __forceinline__ int request_by_length(const AttentionArgs& a, int n) {
@@ -93,8 +99,7 @@ __device__ __forceinline__ int request_by_length(const AttentionArgs& a, int n) 
     if (rank < count) break;
     rank -= count;
   }
-  const bool mine = (same >> lane & 1) && (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0)) == rank;
-  return first + __builtin_ctzll(__ballot(mine) | 1ULL << 63);
+  return first + nth_bit(same, rank);
 }
 // That request's columns from 0 on; false where it has none.
 __device__ __forceinline__ bool whole_request(const AttentionArgs& a, int request, Tile& t) {
@@ -579,17 +584,18 @@ struct Shared {
   float4 stats[4][16 * NT];  // worth of a weight of 1 in powers of two, sum of weights, of weights times minima
 };
 
-// A tile's columns, 16 NT to a wave; where they are fewer than the waves, 2 or 4 waves take the same ones and the steps in turn.
-template <class DT, int D, int NT>
-__device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& t, int columns, int head, int slice, Shared<D, NT>& shared) {
+// A tile's columns.  The four waves are 2^groups_log2 groups, of which each takes 16 NT columns (or, HEADS, all columns of a head of its own, from
+// `first_head` on); the waves of a group take the steps in turn and meet in LDS.
+template <class DT, int D, int NT, bool HEADS>
+__device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& t, int columns, int first_head, int groups_log2, int slice, Shared<D, NT>& shared) {
   constexpr int PER = 16 * NT;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
-  const int groups_log2 = columns <= PER ? 0 : columns <= 2 * PER ? 1 : 2, group = wave & ((1 << groups_log2) - 1);
-  const int first = t.first_column + group * PER;
+  const int group = wave & ((1 << groups_log2) - 1);
+  const int first = HEADS ? t.first_column : t.first_column + group * PER, head = HEADS ? first_head + group : first_head;
   const Steps of_slice = steps_of_slice(a, t, columns, slice);
   if (of_slice.whole && slice > 0) return;
   Columns<D, NT> c;
-  if (first < t.columns) {
+  if (HEADS ? head < a.at.n_kv_heads : first < t.columns) {
     Pages p;
     const Steps steps = load_columns<DT, D, NT>(a, t, first, head, of_slice, lane, c, p);
     attend_steps<DT, D, NT>(a, p, steps.begin + (wave >> groups_log2), steps.end, 2 - groups_log2, lane, c);
@@ -625,9 +631,9 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
   if (groups_log2 == 2) return;
   __syncthreads();
   // sixteen threads to a column
-  const int waves = 4 >> groups_log2, part = threadIdx.x & 15;
-  for (int of_tile = threadIdx.x >> 4; of_tile < columns; of_tile += 16) {
-    const int from = of_tile / PER, at = of_tile % PER;
+  const int waves = 4 >> groups_log2, part = threadIdx.x & 15, all = HEADS ? min(a.at.n_kv_heads - first_head, 1 << groups_log2) * columns : columns;
+  for (int j = threadIdx.x >> 4; j < all; j += 16) {
+    const int from = HEADS ? j / columns : j / PER, at = HEADS ? j - from * columns : j % PER;
     float base = kLowest;
     for (int w = 0; w < waves; ++w) base = fmaxf(base, shared.stats[(w << groups_log2) + from][at].x);
     float sum = 0.0f, minima = 0.0f, v[D / 16] = {};
@@ -642,35 +648,108 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
     }
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) v[k] += minima;
-    const int column = t.first_column + of_tile, row = column / a.group, q_head = head * a.group + column - row * a.group;
+    const int column = t.first_column + (HEADS ? at : j), row = column / a.group, q_head = (HEADS ? first_head + from : first_head) * a.group + column - row * a.group;
     put_values<DT, D>(a, of_slice.whole, t.first_row + row, q_head, slice, part * (D / 16), v, sum);
     if (part == 0) put_sum(a, of_slice.whole, t.first_row + row, q_head, slice, base, sum);
   }
 }
 
-// 64 NT columns of one cache head.  grid = (cache heads x tiles, slices); the last tiles, which see most, first.
-template <class DT, int D, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_many_kernel(AttentionArgs a, int first_tile, int tiles) {
-  __shared__ Shared<D, NT> shared;
-  const int head = blockIdx.x % a.at.n_kv_heads, tile = first_tile + tiles - 1 - (int)(blockIdx.x / a.at.n_kv_heads), slice = blockIdx.y;
-  Tile t;
-  if (!tile_of_batch(a, NT == 1 ? 6 : 7, tile, t)) return;
-  const int columns = min(t.columns - t.first_column, 64 * NT);
-  if (NT > 1 && columns <= 16)
-    attend_tile<DT, D, 1>(a, t, columns, head, slice, reinterpret_cast<Shared<D, 1>&>(shared));
-  else
-    attend_tile<DT, D, NT>(a, t, columns, head, slice, shared);
+// Most requests of a batch whose tiles are ordered by their work.
+constexpr int kMostOrdered = 512;
+struct Ordered {
+  int first_row[kMostOrdered + 1], kv_len[kMostOrdered];
+};
+// The n-th of `tiles` tiles, those with many steps to a wave first: 128 at a time, from the last ones on, in eight classes next to the longest of these.
+// False where it holds no rows.  `per_wave`: columns of a wave.
+__device__ __forceinline__ bool tile_by_work(const AttentionArgs& a, int columns_log2, int per_wave, int tiles, int n, Ordered& o, Tile& t) {
+  const int lane = threadIdx.x & 63;
+  for (int i = threadIdx.x; i <= a.n_reqs; i += 256) {
+    o.first_row[i] = clamp_int(a.q_starts[i], 0, a.n_tokens);
+    if (i < a.n_reqs) o.kv_len[i] = clamp_int(a.kv_lens[i], 0, a.table_width << a.at.page_shift);
+  }
+  __syncthreads();
+  auto tiles_before = [&](int i) { return (int)(((long long)o.first_row[i] * a.group) >> columns_log2) + i; };
+  const int end = tiles - (n & ~127), first = end > 128 ? end - 128 : 0;
+  int of[2], request[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int tile = first + k * 64 + lane;
+    int low = 0, high = a.n_reqs - 1;  // the last request that starts at this tile or before it
+    while (low < high) {
+      const int mid = (low + high + 1) >> 1;
+      if (tiles_before(mid) <= tile)
+        low = mid;
+      else
+        high = mid - 1;
+    }
+    const int rows = max(o.first_row[low + 1] - o.first_row[low], 0), columns = rows * a.group, column = (tile - tiles_before(low)) << columns_log2;
+    const int last_row = (min(column + (1 << columns_log2), columns) - 1) / a.group;
+    const int sees = a.causal ? clamp_int(o.kv_len[low] - rows + last_row + 1, 0, o.kv_len[low]) : o.kv_len[low];
+    // waves that share the columns share the steps
+    const int live = columns - column, of_wave = (a.window > 0 ? min(sees, a.window) : sees) >> (live <= per_wave ? 2 : live <= 2 * per_wave ? 1 : 0);
+    of[k] = tile >= end ? -1 : column < 0 || column >= columns ? 0 : of_wave;
+    request[k] = low;
+  }
+  int most = max(of[0], of[1]);
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) most = max(most, __shfl_xor(most, m));
+  const float classes = 8.0f / (float)(most + 1);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) of[k] = of[k] < 0 ? -1 : min((int)((float)of[k] * classes), 7);
+  int rank = n & 127;
+  unsigned long long one = 0, two = 0;
+  for (int c = 7; c >= 0; --c) {
+    one = __ballot(of[0] == c), two = __ballot(of[1] == c);
+    const int count = __popcll(one) + __popcll(two);
+    if (rank < count) break;
+    rank -= count;
+  }
+  const int in_one = __popcll(one);
+  const bool second = rank >= in_one;
+  const int at = nth_bit(second ? two : one, second ? rank - in_one : rank), tile = first + at + (second ? 64 : 0);
+  t.request = __builtin_amdgcn_readlane(second ? request[1] : request[0], at);
+  // the same in all lanes, and in scalar registers from here on
+  t.first_row = __builtin_amdgcn_readfirstlane(o.first_row[t.request]);
+  t.rows = max(__builtin_amdgcn_readfirstlane(o.first_row[t.request + 1]) - t.first_row, 0);
+  t.columns = t.rows * a.group;
+  t.kv_len = __builtin_amdgcn_readfirstlane(o.kv_len[t.request]);
+  const int before = (int)(((long long)t.first_row * a.group) >> columns_log2) + t.request;
+  if (tile < before || ((long long)(tile - before) << columns_log2) >= t.columns) return false;
+  t.first_column = (tile - before) << columns_log2;
+  return true;
 }
 
-// Requests of up to sixteen columns (more than the hint said: sixteen after sixteen).  grid = (cache heads x requests, slices).
-template <class DT, int D>
+// 64 NT columns of one cache head.  grid = (cache heads x tiles, slices).
+template <class DT, int D, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_many_kernel(AttentionArgs a, int first_tile, int tiles) {
+  constexpr int kLog2 = NT == 1 ? 6 : 7;
+  __shared__ Shared<D, NT> shared;
+  __shared__ Ordered ordered;
+  const int head = blockIdx.x % a.at.n_kv_heads, n = (int)(blockIdx.x / a.at.n_kv_heads), slice = blockIdx.y;
+  Tile t;
+  if (a.ordered) {
+    if (!tile_by_work(a, kLog2, 16 * NT, tiles, n, ordered, t)) return;
+  } else if (!tile_of_batch(a, kLog2, first_tile + tiles - 1 - n, t)) {
+    return;
+  }
+  const int columns = min(t.columns - t.first_column, 64 * NT);
+  if (NT > 1 && columns <= 16)
+    attend_tile<DT, D, 1, false>(a, t, columns, head, 0, slice, reinterpret_cast<Shared<D, 1>&>(shared));
+  else
+    attend_tile<DT, D, NT, false>(a, t, columns, head, columns <= 16 * NT ? 0 : columns <= 32 * NT ? 1 : 2, slice, shared);
+}
+
+// Requests of up to sixteen columns (more than the hint said: sixteen after sixteen), 2^HEADS_LOG2 cache heads to a workgroup.
+// grid = (cache heads / that x requests, slices).
+template <class DT, int D, int HEADS_LOG2>
 __global__ __launch_bounds__(256, 3) void attention_few_kernel(AttentionArgs a, int first_request) {
   __shared__ Shared<D, 1> shared;
-  const int head = blockIdx.x % a.at.n_kv_heads, request = request_by_length(a, first_request + (int)(blockIdx.x / a.at.n_kv_heads)), slice = blockIdx.y;
+  const int blocks = (a.at.n_kv_heads + (1 << HEADS_LOG2) - 1) >> HEADS_LOG2, head = (int)(blockIdx.x % blocks) << HEADS_LOG2;
+  const int request = request_by_length(a, first_request + (int)(blockIdx.x / blocks)), slice = blockIdx.y;
   Tile t;
   if (!whole_request(a, request, t)) return;
   for (; t.first_column < t.columns; t.first_column += kFewColumns) {
-    attend_tile<DT, D, 1>(a, t, min(t.columns - t.first_column, kFewColumns), head, slice, shared);
+    attend_tile<DT, D, 1, (HEADS_LOG2 > 0)>(a, t, min(t.columns - t.first_column, kFewColumns), head, HEADS_LOG2, slice, shared);
     __syncthreads();
   }
 }
@@ -726,11 +805,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, lo
 template <class F>
 hipError_t by_tiles(const AttentionArgs& a, F launch) {
   const long long tiles = a.columns == kFewColumns ? a.n_reqs : attention_tiles(a.n_tokens, a.group, a.n_reqs, a.columns);
+  const int blocks = a.columns == kFewColumns ? (a.at.n_kv_heads + (1 << a.heads_log2) - 1) >> a.heads_log2 : a.at.n_kv_heads;
   // whole sixty-fours of requests
-  const long long share = (1LL << 30) / 256 / a.slices / a.at.n_kv_heads & ~63LL, most = share > 0 ? share : 64;
+  const long long share = (1LL << 30) / 256 / a.slices / blocks & ~63LL, most = share > 0 ? share : 64;
   for (long long first = 0; first < tiles; first += most) {
     const long long n = tiles - first < most ? tiles - first : most;
-    launch(dim3((unsigned)(n * a.at.n_kv_heads), (unsigned)a.slices), (int)first, (int)n);
+    launch(dim3((unsigned)(n * blocks), (unsigned)a.slices), (int)first, (int)n);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
@@ -738,10 +818,17 @@ hipError_t by_tiles(const AttentionArgs& a, F launch) {
 }
 
 template <class DT, int D>
-hipError_t columns_typed(const AttentionArgs& a, hipStream_t st) {
+hipError_t columns_typed(AttentionArgs a, hipStream_t st) {
+  // In the order of their work where the launch goes through the chip a few times at most (eight prompts of up to 1024 rows, 32 heads, 1376 workgroups: 101 -> 86 us; two of
+  // 4095 rows, 4104 workgroups: 848 -> 882); of one request the last tiles are the ones with most work anyway.
+  a.ordered = a.n_reqs > 1 && a.n_reqs <= kMostOrdered;
+  const long long groups = attention_tiles(a.n_tokens, a.group, a.n_reqs, a.columns) * a.at.n_kv_heads * a.slices;
+  a.ordered = a.ordered && groups > 2LL * compute_units() && groups <= 8LL * compute_units();
   return by_tiles(a, [&](dim3 grid, int first, int n) {
-    if (a.columns == kFewColumns)
-      attention_few_kernel<DT, D><<<grid, 256, 0, st>>>(a, first);
+    if (a.columns == kFewColumns && a.heads_log2 == 0)
+      attention_few_kernel<DT, D, 0><<<grid, 256, 0, st>>>(a, first);
+    else if (a.columns == kFewColumns)
+      attention_few_kernel<DT, D, 2><<<grid, 256, 0, st>>>(a, first);
     else if (a.columns == kSomeColumns)
       attention_many_kernel<DT, D, 1><<<grid, 256, 0, st>>>(a, first, n);
     else
