@@ -384,6 +384,53 @@ def test_attention_in_slices(dtype, d, heads, kv_heads, hints):
     check_attention(dtype, d, heads, kv_heads, 16, lens, new, 1, 200, scratch=1 << 24, hints=hints, seed=3)
 
 
+def plan_of(cache, lens, new, heads, hints, scratch=0, window=0, width=None):
+    width = width or max(-(-n // cache.page) for n in lens) + 1
+    b = sg.make_kv_batch(len(lens), sum(new), width, None, None, None, max_q_len=hints[0], max_kv_len=hints[1])
+    return sg.sgmv_plan_attention_q4(cache.c, b, heads, window, 1 << 8 if scratch else None, scratch)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("kv_heads,group,hints,actual", [(5, 1, (1, 40), 1), (5, 2, (1, 600), 1), (6, 3, (5, 40), 5), (5, 3, (1, 30), 9), (7, 17, (0, 0), 1)])
+def test_attention_of_many_short_requests(dtype, kv_heads, group, hints, actual):
+    """More requests than a wave orders at once; a wave to a head (and heads that do not fill the last workgroup); more rows and positions
+    than the hint says."""
+    rng = np.random.default_rng(kv_heads + group)
+    n = 330
+    lens = rng.integers(0, 45, n)
+    lens[7], lens[200] = 300, 0
+    new = np.minimum(rng.integers(0, actual + 1, n), lens + 1)
+    cache = Cache(dtype, 64, kv_heads, 1, 16, 4)
+    plan = plan_of(cache, lens.tolist(), new.tolist(), kv_heads * group, hints)
+    if hints[0] * group in range(1, 17):
+        assert plan.kernel == sg.KERNEL_ATTENTION_FEW
+        assert plan.workgroups == (n * -(-kv_heads // 4) if hints[1] <= 640 else n * kv_heads)
+    check_attention(dtype, 64, kv_heads * group, kv_heads, 16, lens.tolist(), new.tolist(), hints=hints, seed=n)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d,kv_heads,group", [(128, 24, 1), (64, 24, 2), (128, 7, 5)])
+@pytest.mark.parametrize("hint", [0, 130])
+def test_attention_tiles_of_many_prompts(dtype, d, kv_heads, group, hint):
+    """Prompts and single tokens in tiles ordered by their work: whole tiles, ends of 1 to 127 columns (waves that share them), requests without
+    rows, more than 128 tiles."""
+    lens = [130, 1, 33, 64, 0, 17, 100, 40, 65, 3, 129, 48, 31, 96, 20, 77]
+    new = [130, 1, 33, 1, 0, 16, 100, 0, 65, 2, 1, 48, 31, 90, 20, 13]
+    check_attention(dtype, d, kv_heads * group, kv_heads, 16, lens, new, hints=(hint, hint), seed=kv_heads)
+    if kv_heads == 7:
+        check_attention(dtype, d, kv_heads * group, kv_heads, 32, lens * 9, new * 9, hints=(hint, hint), window=50, seed=1)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("hints", [(40, 700), (40, 100000), (1000, 0)])
+def test_attention_of_prompts_in_slices(dtype, hints):
+    """Rows behind long contexts, in slices; rows whose positions fit one slice are written by it, those without any by the join or not at all."""
+    lens, new = [700, 40, 0, 333, 20, 64], [40, 40, 1, 1, 0, 64]
+    for window in (0, 300):
+        check_attention(dtype, 128, 10, 2, 16, lens, new, 1, window, scratch=1 << 25, hints=hints, seed=5)
+    check_attention(dtype, 64, 4, 4, 16, lens, new, 0, 0, scratch=1 << 25, hints=hints, seed=6)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_attention_of_sharp_and_flat_softmaxes(dtype):
     for q_size, scale in ((30.0, 0.3), (1e-3, 1e-3), (0.0, 1.0), (1.0, 1e-30), (100.0, 1.0)):
@@ -509,6 +556,24 @@ def test_attention_one_long_context():
         # the rows read back are rounded to 16 bits, which the kernel's are not: half a step of a score's and a value's parts each
         assert float((out.view(2, 8, d).double() - want).norm() / want.norm()) < 3 * 2.0 ** -8
         assert float((lse.double() - torch.logsumexp(x, -1)).abs().max()) < 0.01
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_odd_positions_of_one_sign(dtype):
+    """Values that are all large and of one sign next to a small spread, and all alike: the codes' sums nearly cancel against the minima."""
+    rng = np.random.default_rng(21)
+    lens = [513, 2]
+    for size, spread in ((100.0, 1.0), (1.0, 0.0), (-50.0, 0.25)):
+        cache, pages, tables = filled_cache(rng, dtype, 128, 1, 16, lens)
+        for r, n in enumerate(lens):
+            p = np.arange(n)
+            v = round16((size + spread * rng.standard_normal((n, 1, 128))).astype(np.float32), dtype)
+            pages.write(1, tables[r, p // 16] * 16 + p % 16, normal(rng, (n, 1, 128), dtype), v)
+        cache.put(pages)
+        q = normal(rng, (5, 3, 128), dtype)
+        out, _ = attend(cache, tables, [0, 3, 5], lens, bits16(q.reshape(5, -1), dtype), 3, 0.05, scratch=1 << 22)
+        want, _, off, weighed = ref.attention(decode64(q, dtype), rows_of(pages, tables, 16), [0, 3, 5], lens, 3, 1, 0.05)
+        assert (np.abs(decode64(host16(out), dtype).reshape(5, 3, 128) - want) <= ref.tolerance(want, off, weighed, dtype)).all()
 
 
 def test_attention_on_another_stream_and_in_a_graph():
