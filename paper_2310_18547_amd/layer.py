@@ -120,6 +120,9 @@ class KvCacheQ4:
             raise ValueError(f"no cache of {n_pages} pages of {page_size} positions, {num_layers} layers of {n_kv_heads} heads of {head_dim}")
         if n_heads <= 0 or n_heads % n_kv_heads or n_reqs <= 0 or n_tokens <= 0 or max_len <= 0:
             raise ValueError(f"{n_heads} heads over {n_kv_heads}, {n_reqs} requests, {n_tokens} rows, {max_len} positions")
+        rope_dim = head_dim if rope_dim is None else rope_dim
+        if rope_dim < 0 or rope_dim > head_dim or rope_dim % 16 or window < 0:
+            raise ValueError(f"{rope_dim} of {head_dim} values rotated (not a multiple of 16 up to that), window {window}")
 
         def ints(*shape, value=0):
             return torch.full(shape, value, dtype=torch.int32, device=device)
@@ -132,13 +135,13 @@ class KvCacheQ4:
         self.free_count, self.status = ints(1, value=n_pages), ints(2)
         self.cache = B.make_kv_cache(dtype, head_dim, n_kv_heads, num_layers, page_size, n_pages, self.pages)
         self.batch = B.make_kv_batch(n_reqs, n_tokens, self.width, self.q_starts, self.lens, self.tables, self.slots, self.positions)
-        rope_dim = head_dim if rope_dim is None else rope_dim
         self.rope = None
         if rope_dim:
             # angles in 64 bits: far positions have many turns behind them
-            angles = torch.arange(max_len, dtype=torch.float64)[:, None] * rope_base ** (-torch.arange(rope_dim // 2, dtype=torch.float64) / (rope_dim // 2))
+            # and for every position that the tables' pages have, in the last one behind max_len too
+            angles = torch.arange(self.width * page_size, dtype=torch.float64)[:, None] * rope_base ** (-torch.arange(rope_dim // 2, dtype=torch.float64) / (rope_dim // 2))
             self.rope_table = torch.cat((angles.cos(), angles.sin()), 1).to(torch.float32).to(device)
-            self.rope = B.make_rope(self.rope_table, max_len, rope_dim, int(adjacent))
+            self.rope = B.make_rope(self.rope_table, self.width * page_size, rope_dim, int(adjacent))
         self.q = torch.zeros(n_tokens, n_heads * head_dim, dtype=kind, device=device)    # rotated
         self.out = torch.zeros(n_tokens, n_heads * head_dim, dtype=kind, device=device)
         self.hint(max_q_len, max_kv_len)
@@ -297,4 +300,7 @@ class Q8Layer(LoraLayer):
         if (cache.kind, cache.n_tokens, cache.n_heads * cache.head_dim, cache.n_kv_heads * cache.head_dim) != (self.kind, self.n_tokens, self.h, self.h):
             raise ValueError(f"a cache of {cache.n_tokens} rows of {cache.n_heads} / {cache.n_kv_heads} heads of {cache.head_dim} {cache.kind}, not of "
                              f"{self.n_tokens} rows of {self.h} {self.kind}")
+        if cache.pages.device != self.x.device or not 0 <= layer_idx < cache.cache.num_layers:
+            raise ValueError(f"layer {layer_idx} on {self.x.device}: the cache has {cache.cache.num_layers} on {cache.pages.device}")
+        self._apart(residual, (cache.q, cache.out), "residual")
         return self.finish(cache.run(layer_idx, *self.qkv(x, residual, layer_idx, scale, stream), stream), residual, layer_idx, scale, stream)

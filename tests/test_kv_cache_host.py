@@ -26,15 +26,15 @@ def test_cache_and_its_first_state():
     t = _cache()
     assert t.width == 4 and t.tables.shape == (3, 4) and int(t.free_count) == 6 and t.free_pages.tolist() == list(range(6))
     assert t.pages.shape == (6, LAYERS * (16 * 64 + 128)) and t.scale == 64 ** -0.5
-    assert t.rope_table.shape == (50, 64) and t.rope_table[0].tolist() == [1.0] * 32 + [0.0] * 32
+    assert t.rope_table.shape == (64, 64) and t.rope.rows == 64 and t.rope_table[0].tolist() == [1.0] * 32 + [0.0] * 32
     assert abs(float(t.rope_table[49, 32]) - torch.tensor(49.0, dtype=torch.float64).sin().item()) < 1e-7
     t.hint(1, 77)
     assert (t.batch.max_q_len, t.batch.max_kv_len) == (1, 77)
-    assert _cache(rope_dim=0).rope is None and _cache(rope_dim=32).rope_table.shape == (50, 32)
+    assert _cache(rope_dim=0).rope is None and _cache(rope_dim=32).rope_table.shape == (64, 32)
 
 
 @pytest.mark.parametrize("wrong", [dict(head_dim=96), dict(page_size=20), dict(n_pages=0), dict(n_heads=3, n_kv_heads=2), dict(n_reqs=0),
-                                   dict(n_tokens=0), dict(max_len=0), dict(n_heads=0)])
+                                   dict(n_tokens=0), dict(max_len=0), dict(n_heads=0), dict(rope_dim=24), dict(rope_dim=80), dict(rope_dim=-16), dict(window=-1)])
 def test_caches_that_are_refused(wrong):
     with pytest.raises(ValueError):
         _cache(**wrong)
@@ -73,4 +73,8 @@ def test_a_whole_layer(kv_calls):
     for wrong in (dict(n_tokens=N + 1), dict(dtype=sg.BF16), dict(head_dim=128), dict(n_heads=2)):
         with pytest.raises(ValueError):
             layer.run(_rows(), residual, 0, _cache(**wrong))
+    cache = _cache()
+    for residual, layer_idx in ((cache.out, 0), (cache.q, 0), (_rows(), LAYERS), (_rows(), -1)):
+        with pytest.raises(ValueError):
+            layer.run(_rows(), residual, layer_idx, cache)
     assert len(kv_calls) == before and FFN > H
