@@ -112,7 +112,7 @@ struct Estimate {
 // `room`: bytes of workspace.
 AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads, int32_t window, size_t room) {
   const long long group = n_heads / c->n_kv_heads, covered = (long long)b->table_width * c->page_size;
-  const long long rows = b->max_q_len > 0 ? b->max_q_len : (b->n_tokens + b->n_reqs - 1LL) / b->n_reqs;
+  const long long rows = b->max_q_len > 0 ? (b->max_q_len < b->n_tokens ? b->max_q_len : b->n_tokens) : (b->n_tokens + b->n_reqs - 1LL) / b->n_reqs;
   long long longest = b->max_kv_len > 0 && b->max_kv_len < covered ? b->max_kv_len : covered;
   if (window > 0 && longest > window + rows) longest = window + rows;
   const long long steps = longest > 0 ? (longest + kStepPositions - 1) / kStepPositions : 1;

@@ -28,8 +28,10 @@ namespace {
 // Below every score, and what a column's maximum is before it has seen one.
 constexpr float kLowest = -3.0e38f;
 // The weights are 2^unit larger than their definition, so that the largest one times the largest scale of v stays below 2^11 (binary16 has
-// all of its 11 bits down to 2^-25 of that), and below 2^15 while a column's maximum is up to 2^4 behind.
-constexpr int kWeightTop = 11;
+// all of its 11 bits down to 2^-25 of that), and below 2^15 while a column's maximum is up to 2^4 behind.  Minima count as scales of 2^-60
+// of their size, so that 2^30 positions' stay below 2^105 in sum where v is constant, and with neither the weights themselves below 2^124.
+constexpr int kWeightTop = 11, kMostUnit = 90;
+constexpr float kMinimum = 0x1p-60f;
 constexpr float kBehind = 4.0f;
 
 // Codes of a word's halves as binary16 operands of 2^-20 each: values n and n + 4 of part n.
@@ -257,7 +259,8 @@ __device__ __forceinline__ void load_query(const AttentionArgs& a, const uint16_
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
   out.sum = sum * 0x1p-20f;
-  out.factor = fits ? ldexpf(a.scale * 1.44269504088896341f, 20 - up) : __uint_as_float(0x7FC00000u);
+  // (not zero: times the -infinity of a hidden position that would be NaN)
+  out.factor = fits ? fmaxf(ldexpf(a.scale * 1.44269504088896341f, 20 - up), 0x1p-126f) : __uint_as_float(0x7FC00000u);
 }
 
 // First of the values whose row 4 g + i of output tile j a lane receives: value_of + j.
@@ -279,7 +282,7 @@ struct Columns {
   float minima[NT];  // of the weights times v's minima
   f32x4 acc[NT][D / 16];  // of the weights times v's codes and scales, times 2^-20
   int unit;
-  float limit;       // scales of v above it lower the unit; infinity in lanes that hold k's
+  float limit;       // scales and minima of v above it (Scores::size) lower the unit; infinity in lanes that hold k's
 };
 template <int D, int NT>
 __device__ __forceinline__ void start_columns(Columns<D, NT>& c, int lane) {
@@ -290,7 +293,7 @@ __device__ __forceinline__ void start_columns(Columns<D, NT>& c, int lane) {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) c.acc[n][j] = f32x4{};
   }
-  c.unit = 100;
+  c.unit = kMostUnit;
   c.limit = lane & 8 ? 0.0f : __uint_as_float(0x7F800000u);
 }
 
@@ -300,7 +303,7 @@ __device__ __forceinline__ void raise(Columns<D, NT>& c, const float (&highest)[
   float s = lane & 8 ? scale : 0.0f;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) s = fmaxf(s, __shfl_xor(s, m));
-  const int fits = min(kWeightTop - ((int)(__float_as_uint(s) >> 23) - 126), 100);  // s < 2^(kWeightTop - fits)
+  const int fits = min(kWeightTop - ((int)(__float_as_uint(s) >> 23) - 126), kMostUnit);  // s < 2^(kWeightTop - fits)
   const int unit = min(c.unit, fits);
   const float by = ldexpf(1.0f, unit - c.unit);
   c.unit = unit;
@@ -326,7 +329,7 @@ template <int NT>
 struct Scores {
   float x[NT][8], highest[NT];
   uint32_t sees[NT];  // a bit for every position that the column sees
-  float scale, low, size;
+  float scale, low, size;  // size: what the weights are to fit
   bool above;         // of a bar or a limit: raise() is due
 };
 // Scores of the 32 positions whose keys are in `s`.  MASKED: some column does not see all of them, or a tile is not `there`.
@@ -339,7 +342,7 @@ __device__ __forceinline__ void score_step(const Held<D>& s, int first_pos, uint
     const int pos = first_pos + (i & 4) * 4 + g * 4 + (i & 3);
     if (pos < c.some.low || pos >= c.some.high || !(there >> (i >> 2 & 1) & 1u)) r.scale = r.low = 0.0f;
   }
-  r.size = r.scale;
+  r.size = fmaxf(r.scale, fabsf(r.low) * kMinimum);
   const bool down = (i & 9) == 9;
   r.low = fmaf(r.scale, down ? 15.0f : 0.0f, r.low);
   r.scale = down ? -r.scale : r.scale;

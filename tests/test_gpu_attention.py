@@ -201,7 +201,8 @@ def random_step(rng, n, page, longest, tokens, over=0.2, spare=5):
 
 
 @pytest.mark.parametrize("n,page,longest,tokens", [(1, 16, 0, 1), (1, 16, 40, 500), (3, 32, 100, 2), (64, 16, 300, 1), (65, 64, 300, 90),
-                                                   (1023, 16, 60, 3), (1025, 16, 90, 2), (3000, 32, 500, 1), (130, 256, 1000, 200)])
+                                                   (1023, 16, 60, 3), (1025, 16, 90, 2), (3000, 32, 500, 1), (130, 256, 1000, 200),
+                                                   (4097, 16, 40, 1), (5000, 16, 20, 3), (9000, 32, 60, 2)])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_assign(n, page, longest, tokens, in_place):
     rng = np.random.default_rng(n + page)
@@ -576,6 +577,44 @@ def test_attention_odd_positions_of_one_sign(dtype):
         assert (np.abs(decode64(host16(out), dtype).reshape(5, 3, 128) - want) <= ref.tolerance(want, off, weighed, dtype)).all()
 
 
+@pytest.mark.parametrize("dtype,value,lens", [("f16", 40000.0, [9000, 33]), ("f16", -65504.0, [8200]), ("bf16", 1e9, [513]), ("bf16", -1e30, [513, 40]),
+                                              ("bf16", 2e38, [300]), ("bf16", 0.0, [513, 1]), ("f16", 0.0, [40])])
+def test_attention_constant_values(dtype, value, lens):
+    """Rows of v without a scale: nothing but minima, up to the type's largest."""
+    rng = np.random.default_rng(7)
+    cache, pages, tables = filled_cache(rng, dtype, 64, 1, 16, lens)
+    value = decode64(round16(np.full(1, value, np.float32), dtype), dtype)[0]
+    for r, n in enumerate(lens):
+        p = np.arange(n)
+        pages.write(1, tables[r, p // 16] * 16 + p % 16, normal(rng, (n, 1, 64), dtype), round16(np.full((n, 1, 64), value, np.float32), dtype))
+    cache.put(pages)
+    new = [1] * len(lens)
+    starts = np.concatenate(([0], np.cumsum(new)))
+    q = normal(rng, (len(lens), 4, 64), dtype)
+    for scratch in (0, 1 << 22):
+        out, lse = attend(cache, tables, starts, lens, bits16(q.reshape(len(lens), -1), dtype), 4, 0.125, scratch=scratch)
+        want, want_lse, off, _ = ref.attention(decode64(q, dtype), rows_of(pages, tables, 16), starts, lens, 4, 1, 0.125)
+        got = decode64(host16(out), dtype).reshape(want.shape)
+        # the same weights in the sum and under it, n additions of fp32 each
+        assert (np.abs(got - value) <= abs(value) * (ref.HALF_STEP[dtype] + 2.0 ** -24 * (2 * max(lens) + 16))).all()
+        assert (np.abs(host(lse).astype(np.float64) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
+
+
+@pytest.mark.parametrize("scratch", [0, 1 << 20])
+def test_attention_tiny_scores_and_a_hidden_page(scratch):
+    """Scores so small that their factor is no number of fp32, next to a page that is not of the cache: all weights alike, its own nothing."""
+    rng = np.random.default_rng(8)
+    lens = [256]
+    cache, pages, tables = filled_cache(rng, "bf16", 128, 1, 16, lens)
+    tables[0, 3] = -1
+    q = normal(rng, (1, 2, 128), "bf16", 1e-36)
+    out, lse = attend(cache, tables, [0, 1], lens, bits16(q.reshape(1, -1), "bf16"), 2, 1e-20, scratch=scratch)
+    hidden = lambda r: np.arange(256) // 16 == 3
+    want, want_lse, off, spread = ref.attention(decode64(q, "bf16"), rows_of(pages, tables, 16), [0, 1], lens, 2, 1, 1e-20, hidden=hidden)
+    assert (np.abs(decode64(host16(out), "bf16").reshape(want.shape) - want) <= ref.tolerance(want, off, spread, "bf16")).all()
+    assert (np.abs(host(lse) - want_lse) <= 1e-5).all()
+
+
 def test_attention_on_another_stream_and_in_a_graph():
     rng = np.random.default_rng(12)
     lens, new = [300, 40, 17], [1, 5, 1]
@@ -607,6 +646,51 @@ def test_attention_on_another_stream_and_in_a_graph():
             g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager) and torch.equal(other, sharp), i
+
+
+def test_two_calls_at_once_on_streams_of_their_own():
+    """The same cache and batch, workspaces apart."""
+    rng = np.random.default_rng(14)
+    lens = [3000, 2500]
+    cache, pages, tables = filled_cache(rng, "bf16", 128, 2, 16, lens)
+    q = bits16(normal(rng, (2, 1024), "bf16"), "bf16")
+    scales = (0.05, 0.2)
+    want = [attend(cache, tables, [0, 1, 2], lens, q, 8, s, scratch=1 << 20, hints=(1, 3000), lse=False)[0] for s in scales]
+    q_starts, kv_lens, t = ints([0, 1, 2]), ints(lens), ints(tables)
+    b = sg.make_kv_batch(2, 2, tables.shape[1], q_starts, kv_lens, t, max_q_len=1, max_kv_len=3000)
+    assert sg.sgmv_plan_attention_q4(cache.c, b, 8, 0, 1 << 8, 1 << 20).slices > 1
+    streams, works, outs = ([f() for _ in scales] for f in (torch.cuda.Stream, lambda: torch.empty(1 << 20, dtype=torch.uint8, device="cuda"),
+                                                           lambda: torch.zeros(2, 1024, dtype=torch.bfloat16, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, work, out, scale in zip(streams, works, outs, scales):
+            sg.sgmv_attention_q4(cache.c, b, 1, out, None, q, 8, 1024, 1024, scale, 1, 0, work, 1 << 20, stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_pages_far_apart():
+    """A cache whose pages lie 2^30 bytes from one another: what it holds and gives is what a dense one does."""
+    rng = np.random.default_rng(15)
+    n_pages, page, d, stride = 6, 16, 64, 1 << 30
+    store = torch.empty((n_pages - 1) * stride + (1 << 20), dtype=torch.uint8, device="cuda")
+    far = sg.make_kv_cache(sg.F16, d, 2, 3, page, n_pages, store, stride)
+    dense = Cache("f16", d, 2, 3, page, n_pages)
+    n, new = 90, 20
+    tables = np.array([[5, 0, 4, 1, 3, 2]])
+    p = np.arange(n)
+    slots, starts, lens, t = ints(tables[0, p // page] * page + p % page), ints([0, new]), ints([n]), ints(tables)
+    k, v = (bits16(normal(rng, (n, 2 * d), "f16"), "f16") for _ in range(2))
+    q = bits16(normal(rng, (new, 4 * d), "f16"), "f16")
+    rows, results = sg.make_kv_batch(1, n, 6, None, None, None, slots), []
+    for c in (far, dense.c):
+        sg.sgmv_kv_append_q4(c, rows, 2, None, None, k, v, 4, 4 * d, 4 * d, 2 * d)
+        out, gk, gv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+        sg.sgmv_attention_q4(c, sg.make_kv_batch(1, new, 6, starts, lens, t), 2, out, None, q, 4, 4 * d, 4 * d, 0.125)
+        sg.sgmv_kv_read_q4(c, 2, gk, gv, 2 * d, slots, n)
+        torch.cuda.synchronize()
+        results.append((out, gk, gv))
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and bool(results[0][0].abs().sum() > 0)
 
 
 def test_a_served_batch_step_after_step():
