@@ -179,26 +179,28 @@ __device__ __forceinline__ Lane<D> offsets_of(int lane) {
   const uint32_t g = (uint32_t)lane >> 4, i = (uint32_t)lane & 15;
   return {i * (D / 2) + g * (D / 8), 8 * D + g * (2 * D) + (D == 128 ? i : i & 7) * 16, 16 * D + (i & 8) * 8 + g * 16 + (i & 3) * 4, (i & 4) != 0};
 }
-template <int D>
+// ONCE: nobody else reads these tiles, so they pass the caches by (few columns: 64 requests of 512 to 2048 positions 80 -> 75 us, 131 000 positions 37 -> 35;
+// but tiles of prompts, which meet there: 84 -> 89).
+template <int D, bool ONCE>
 __device__ __forceinline__ void load_k(const Place& at, const Lane<D>& lane, Held<D>& s) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const __amdgpu_buffer_rsrc_t tile = make_buffer(h ? at.second : at.first, tile_bytes(D));
     if constexpr (D == 128) {
-      const uint4 w = buffer_load128<0>(tile, lane.k);
+      const uint4 w = buffer_load128<ONCE ? kNonTemporal : 0>(tile, lane.k);
       s.k[h][0] = w.x, s.k[h][1] = w.y, s.k[h][2] = w.z, s.k[h][3] = w.w;
     } else {
-      const uint2 w = buffer_load64_at<0>(tile, lane.k, 0);
+      const uint2 w = buffer_load64_at<ONCE ? kNonTemporal : 0>(tile, lane.k, 0);
       s.k[h][0] = w.x, s.k[h][1] = w.y;
     }
   }
   const uint8_t *first = at.first, *second = at.second;
   s.pair = *reinterpret_cast<const uint32_t*>((lane.second ? second : first) + (size_t)lane.pair);
 }
-template <int D>
+template <int D, bool ONCE>
 __device__ __forceinline__ void load_v(const Place& at, const Lane<D>& lane, Held<D>& s) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) s.v[h] = buffer_load128<0>(make_buffer(h ? at.second : at.first, tile_bytes(D)), lane.v);
+  for (int h = 0; h < 2; ++h) s.v[h] = buffer_load128<ONCE ? kNonTemporal : 0>(make_buffer(h ? at.second : at.first, tile_bytes(D)), lane.v);
 }
 
 // The value of the i-th of a lane's sixteen neighbours.
@@ -451,7 +453,7 @@ __device__ __forceinline__ void weigh_step(const Held<D>& s, int lane, Scores<NT
 }
 
 // The next step's keys are loaded as soon as the scores are there, its values after the products with this one's.
-template <class DT, int D, int NT>
+template <class DT, int D, int NT, bool ONCE>
 __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages& p, int begin, int end, int stride_log2, int lane, Columns<D, NT>& c) {
   if (begin >= end) return;
   const Lane<D> offsets = offsets_of<D>(lane);
@@ -469,8 +471,8 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
   // pages are looked up two steps ahead of their use: a scalar load's wait is for all of them
   Looked pages = look_up(a, p, step_at(1));
   Place at = place_of<D>(a, p, step_at(0), look_up(a, p, step_at(0))), next;
-  load_k<D>(at, offsets, held);
-  load_v<D>(at, offsets, held);
+  load_k<D, ONCE>(at, offsets, held);
+  load_v<D, ONCE>(at, offsets, held);
   next = place_of<D>(a, p, step_at(1), pages);
   pages = look_up(a, p, step_at(2));
   int n = 0;
@@ -483,10 +485,10 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
   Scores<NT> r;
   while (n < ends) {
     score_step<DT, D, NT, true>(held, step_at(n) * kStepPositions, at.there, lane, c, r);
-    load_k<D>(next, offsets, held);
+    load_k<D, ONCE>(next, offsets, held);
     if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
     weigh_step<DT, D, NT, true>(held, lane, r, c);
-    load_v<D>(next, offsets, held);
+    load_v<D, ONCE>(next, offsets, held);
     on();
   }
   while (n < count) {
@@ -494,9 +496,9 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
     score_step<DT, D, NT, false>(held, 0, at.there, lane, c, r);
     if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
     for (;;) {
-      load_k<D>(next, offsets, held);
+      load_k<D, ONCE>(next, offsets, held);
       weigh_step<DT, D, NT, false>(held, lane, r, c);
-      load_v<D>(next, offsets, held);
+      load_v<D, ONCE>(next, offsets, held);
       on();
       if (n >= count) break;
       score_step<DT, D, NT, false>(held, 0, at.there, lane, c, r);
@@ -589,7 +591,7 @@ struct Shared {
 
 // A tile's columns.  The four waves are 2^groups_log2 groups, of which each takes 16 NT columns (or, HEADS, all columns of a head of its own, from
 // `first_head` on); the waves of a group take the steps in turn and meet in LDS.
-template <class DT, int D, int NT, bool HEADS>
+template <class DT, int D, int NT, bool HEADS, bool ONCE>
 __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& t, int columns, int first_head, int groups_log2, int slice, Shared<D, NT>& shared) {
   constexpr int PER = 16 * NT;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
@@ -601,7 +603,7 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
   if (HEADS ? head < a.at.n_kv_heads : first < t.columns) {
     Pages p;
     const Steps steps = load_columns<DT, D, NT>(a, t, first, head, of_slice, lane, c, p);
-    attend_steps<DT, D, NT>(a, p, steps.begin + (wave >> groups_log2), steps.end, 2 - groups_log2, lane, c);
+    attend_steps<DT, D, NT, ONCE>(a, p, steps.begin + (wave >> groups_log2), steps.end, 2 - groups_log2, lane, c);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float sum = of_column(c.sum[n]), minima = of_column(c.minima[n]);
@@ -737,9 +739,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_many_kernel(At
   }
   const int columns = min(t.columns - t.first_column, 64 * NT);
   if (NT > 1 && columns <= 16)
-    attend_tile<DT, D, 1, false>(a, t, columns, head, 0, slice, reinterpret_cast<Shared<D, 1>&>(shared));
+    attend_tile<DT, D, 1, false, false>(a, t, columns, head, 0, slice, reinterpret_cast<Shared<D, 1>&>(shared));
   else
-    attend_tile<DT, D, NT, false>(a, t, columns, head, columns <= 16 * NT ? 0 : columns <= 32 * NT ? 1 : 2, slice, shared);
+    attend_tile<DT, D, NT, false, false>(a, t, columns, head, columns <= 16 * NT ? 0 : columns <= 32 * NT ? 1 : 2, slice, shared);
 }
 
 // Requests of up to sixteen columns (more than the hint said: sixteen after sixteen), 2^HEADS_LOG2 cache heads to a workgroup.
@@ -752,7 +754,7 @@ __global__ __launch_bounds__(256, 3) void attention_few_kernel(AttentionArgs a, 
   Tile t;
   if (!whole_request(a, request, t)) return;
   for (; t.first_column < t.columns; t.first_column += kFewColumns) {
-    attend_tile<DT, D, 1, (HEADS_LOG2 > 0)>(a, t, min(t.columns - t.first_column, kFewColumns), head, HEADS_LOG2, slice, shared);
+    attend_tile<DT, D, 1, (HEADS_LOG2 > 0), true>(a, t, min(t.columns - t.first_column, kFewColumns), head, HEADS_LOG2, slice, shared);
     __syncthreads();
   }
 }

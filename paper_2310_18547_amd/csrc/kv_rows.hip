@@ -8,8 +8,9 @@
 // codes.  Every product and sum of the rotation is rounded to fp32 by itself (no fused multiply-add) and quotients are correctly rounded, so
 // that a code next to the border of two does not depend on how the compiler joins operations.
 //
-// Bound by memory: 4184 rows of 64 query and 8 cache heads, 158 MB there and back, 36 us (4.4 TB/s; a copy of 1 GiB reaches 5.1; 47 us where the
-// lanes of a head load its cosines and sines each time, with divisions); their rows back 7.2 us; one row of 96 heads 4.2 us, its launch.
+// Bound by memory: 4184 rows of 64 query and 8 cache heads, 158 MB there and back, 32 us (4.9 TB/s; a copy of 1 GiB reaches 5.1; 36 us with loads that stay in
+// the caches, 47 where the lanes of a head load its cosines and sines each time, with divisions); their rows back 7.2 us; one row of 96
+// heads 4.2 us, its launch.
 #include "device_common.h"
 #include "kv.h"
 
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a, int firs
       const int unit = base + k * GROUPS + group, head = unit - a.n_heads;
       words[k] = make_uint4(0, 0, 0, 0);
       if (unit < end)
-        words[k] = load128(head < 0 ? q_row + unit * D : head < a.at.n_kv_heads ? k_row + head * D : v_row + (head - a.at.n_kv_heads) * D);
+        words[k] = load128_stream(head < 0 ? q_row + unit * D : head < a.at.n_kv_heads ? k_row + head * D : v_row + (head - a.at.n_kv_heads) * D);
     }
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
