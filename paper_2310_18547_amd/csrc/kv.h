@@ -61,8 +61,8 @@ struct KvReadArgs {
 };
 hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st);
 
-// Columns of an attention workgroup's tile: rows x query heads of one cache head's group, row by row.
-constexpr int kFewColumns = 16, kSomeColumns = 64, kManyColumns = 128;
+// Columns of an attention workgroup's tile: rows x query heads of one cache head's group, row by row; of all of a request, or of a tile of the batch at most.
+constexpr int kFewColumns = 16, kManyColumns = 128;
 // Positions of one step of a wave.
 constexpr int kStepPositions = 32;
 struct AttentionArgs {
@@ -72,8 +72,9 @@ struct AttentionArgs {
   int n_heads, group, n_reqs, n_tokens, table_width;
   int causal, window;
   float scale;
-  int columns;               // one of the three
-  int heads_log2;            // kFewColumns: cache heads of a workgroup, one (whose steps its waves share) or 2^2 (a wave each)
+  bool few;                  // whole requests, kFewColumns at a time; else tiles of the batch
+  int columns_log2;          // of a tile, 4 to 7
+  int heads_log2;            // few: cache heads of a workgroup, one (whose steps its waves share) or 2^2 (a wave each)
   uint16_t* out;
   float* lse;
   const uint16_t* q;

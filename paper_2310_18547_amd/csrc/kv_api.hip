@@ -86,27 +86,41 @@ int check_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_he
 }
 
 struct AttentionPlan {
-  int columns, heads_log2, slices, slice_steps;
+  bool few;
+  int columns_log2, heads_log2, slices, slice_steps;
   long long workgroups;
 };
 size_t slice_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_heads) {
   return (size_t)b->n_tokens * (size_t)n_heads * (4 * (size_t)c->head_dim + 8);
 }
-// Time of an attention launch in us, to choose the kernel and the slices by.  One, two and three workgroups to a unit take 1.2, 1.6 and 2.4 us for a step
-// of 32 positions of sixteen columns (the loads; 131 000 positions in 48, 64 and 96 slices: 1.5, 1.8, 2.4), 1.4 where the keys come from the
-// caches, and 1.6 for thirty-two columns to a wave; a workgroup's lookups, queries and end take 4 us (64 requests of 512 to 2048 positions, 32
-// heads: 80 us whole, 133 in six slices), and a batch's last round is half empty; a join 3 us and its sums' way there and back at 4 TB/s.
+// Time of an attention launch in us, to choose the kernel, the tiles and the slices by.
+//
+// Few columns: one, two and three workgroups to a unit take 1.2, 1.6 and 2.4 us for a step of 32 positions (the loads; 131 000 positions in 48, 64 and
+// 96 slices: 1.5, 1.8, 2.4), a workgroup's lookups, queries and end 4 us (64 requests of 512 to 2048 positions, 32 heads: 80 us whole, 133 in
+// six slices), and a batch's last round is half empty.
+// Tiles: 1.1 us a step and 4 us around them while tiles are few (1.15 and 6 where a wave has 32 columns), 1.4 (1.6) and 6.5 us where they queue
+// for units.  300 rows, 32 heads, in tiles of 16 / 32 / 64 / 128: 10 / 11 / 15 / 19 us; 600 and 600 rows 36 / 32 / 28 / 35; 8 prompts of up to 1024
+// 127 / 101 / 104 / 85; 453 rows next to 64 single tokens, 8 heads shared by 4 each, 36 / 30 / 26 / 32.
+// A join takes 3 us and its sums' way there and back at 4 TB/s.
 struct Estimate {
-  double steps, mean_steps;  // of the longest tile, and of an average one
   double rows, heads, tile_bytes, units;
-  // workgroups of a slice; waves of a workgroup that share the steps, in a tile of the longest request and in an average one
-  double us(int columns, double groups, double share, double mean_share, int slices) const {
-    const double resident = columns == kManyColumns ? 2 : 3, total = groups * slices, slots = resident * units;
-    const int waves = total >= slots ? (int)resident : (int)((total + units - 1) / units);
-    const double step = columns == kFewColumns ? (waves == 1 ? 1.2 : waves == 2 ? 1.6 : 2.4) : columns == kSomeColumns ? 1.4 : 1.6;
-    const double longest = (double)(long long)(steps / slices / share + 0.999) * step + 4.0;
-    const double all = total > slots ? (total / slots + 0.5) * (mean_steps / slices / mean_share * step + 4.0) : 0.0;
-    return 1.5 + (longest > all ? longest : all) + (slices > 1 ? 3.0 + rows * heads * slices * tile_bytes / 2 / 4e6 : 0.0);
+  double join(int slices) const { return slices > 1 ? 3.0 + rows * heads * slices * tile_bytes / 2 / 4e6 : 0.0; }
+  // `groups` workgroups of a slice, of at most `steps` steps to a wave
+  double few(double groups, double steps, double mean_steps, int slices) const {
+    const double total = groups * slices, slots = 3 * units;
+    const int waves = total >= slots ? 3 : (int)((total + units - 1) / units);
+    const double step = waves == 1 ? 1.2 : waves == 2 ? 1.6 : 2.4;
+    const double longest = (double)(long long)(steps + 0.999) * step + 4.0;
+    const double all = total > slots ? (total / slots + 0.5) * (mean_steps * step + 4.0) : 0.0;
+    return 1.5 + (longest > all ? longest : all) + join(slices);
+  }
+  // `steps` of all tiles together
+  double many(int columns, double groups, double steps, double all_steps, int slices) const {
+    const bool wide = columns == kManyColumns;
+    const double total = groups * slices, slots = (wide ? 2 : 3) * units;
+    const double longest = (double)(long long)(steps + 0.999) * (wide ? 1.15 : 1.1) + (wide ? 6.0 : 4.0);
+    const double all = total > slots ? (total / slots + 0.4) * (all_steps / groups * (wide ? 1.6 : 1.4) + 6.5) : 0.0;
+    return 1.5 + (longest > all ? longest : all) + join(slices);
   }
 };
 // `room`: bytes of workspace.
@@ -118,34 +132,44 @@ AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int
   const long long steps = longest > 0 ? (longest + kStepPositions - 1) / kStepPositions : 1;
   const long long fit = (long long)(room / slice_bytes(c, b, n_heads)), most = fit < 1 ? 1 : fit < kMostSlices ? fit : kMostSlices;
   Estimate e = {};
-  // Prompts next to single tokens are taken for new ones, shorter than the longest context, unless that is much longer than a prompt (a part of a long one
-  // may then stand at its end, and slices that nobody needs cost less than one workgroup that goes through all of it).
-  const bool new_prompts = rows * group > kFewColumns && b->n_tokens < rows * b->n_reqs / 2 && longest <= 4 * rows;
-  e.steps = new_prompts ? (double)((rows + kStepPositions - 1) / kStepPositions) : (double)steps;
-  e.mean_steps = (double)steps - (double)(rows < longest ? rows : longest) / (2 * kStepPositions);
   e.rows = b->n_tokens;
   e.heads = n_heads;
   e.tile_bytes = tile_bytes(c->head_dim);
   e.units = compute_units();
   AttentionPlan p = {};
+  p.few = rows * group <= kFewColumns;
   double best = 0;
   static const int kSlices[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
-  static const int kColumns[] = {kFewColumns, kSomeColumns, kManyColumns};
-  for (const int columns : kColumns) {
-    if ((columns == kFewColumns) != (rows * group <= kFewColumns)) continue;
+  const double seen = (double)steps - (double)(rows < longest ? rows : longest) / (2 * kStepPositions);  // by an average row
+  // Requests with the most rows, if the others have one each (over 0.6 of the longest context on average).  Prompts next to single tokens are taken for new ones, shorter than the longest context, unless
+  // that is much longer than a prompt (a part of a long one may then stand at its end, and slices that nobody needs cost less than one
+  // workgroup that goes through all of it).
+  const long long more = b->n_tokens - b->n_reqs, full = rows > 1 ? (more + rows - 2) / (rows - 1) : b->n_reqs;
+  const long long prompts = full < 1 ? 1 : full < b->n_reqs ? full : b->n_reqs, others = b->n_reqs - prompts;
+  const bool fresh = prompts <= b->n_reqs / 2 && longest <= 6 * rows;
+  const double prompt_steps = fresh ? (double)((rows + kStepPositions - 1) / kStepPositions) : (double)steps, prompt_mean = fresh ? prompt_steps / 2 : seen;
+  for (int log2 = 4; log2 <= (p.few ? 4 : 7); ++log2) {
+    const int columns = 1 << log2;
     // tiles of requests that all have the most rows, or of the whole batch if that is less
-    const long long all = columns == kFewColumns ? b->n_reqs : attention_tiles(b->n_tokens, (int)group, b->n_reqs, columns);
-    const long long busiest = b->n_reqs * ((rows * group + columns - 1) / columns);
-    const long long groups = (all < busiest ? all : busiest) * c->n_kv_heads;
+    const long long all = p.few ? b->n_reqs : attention_tiles(b->n_tokens, (int)group, b->n_reqs, columns);
+    const long long busiest = b->n_reqs * ((rows * group + columns - 1) / columns), tiles = all < busiest ? all : busiest;
     const long long per_wave = columns == kManyColumns ? 32 : 16;
     auto share_of = [&](long long live) { return live <= per_wave ? 4 : live <= 2 * per_wave ? 2 : 1; };
-    const int share = share_of(rows * group < columns ? rows * group : columns), mean_share = share_of(b->n_tokens * group * c->n_kv_heads / groups);
+    const int share = share_of(rows * group < columns ? rows * group : columns), other_share = share_of(group < columns ? group : columns);
+    const long long of_prompts = tiles > others ? tiles - others : 0;
+    const double groups = (double)(tiles * c->n_kv_heads);
     for (const int slices : kSlices) {
       if (slices > most || (slices > 1 && slices * share > steps)) break;
-      const double us = e.us(columns, (double)groups, share, mean_share, slices);
-      if (p.columns != 0 && us >= best) continue;
+      double us;
+      if (p.few) {
+        us = e.few(groups, (double)steps / slices / share, seen / slices / share, slices);
+      } else {
+        const double one = prompt_steps / share, other = others > 0 ? (double)steps / other_share : 0.0;
+        us = e.many(columns, groups, (one > other ? one : other) / slices, (double)c->n_kv_heads * ((double)of_prompts * prompt_mean / share + (double)others * other * 0.6) / slices, slices);
+      }
+      if (best > 0 && us >= best) continue;
       best = us;
-      p.columns = columns;
+      p.columns_log2 = log2;
       p.slices = slices;
       p.slice_steps = (int)((steps + slices - 1) / slices);
       p.workgroups = all * c->n_kv_heads * slices;
@@ -153,7 +177,7 @@ AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int
   }
   // A wave to a head saves its waves' common start and end where there are heads enough and all contexts are short (64 requests of 32 heads, a head to a
   // workgroup / to a wave: 128 positions 21.9 / 12.9 us, 512 40.7 / 33.4, 1024 63.7 / 58.3; but 512 to 2048 81 / 91, where the longest are left running).
-  if (p.columns == kFewColumns && p.slices == 1 && steps <= 20 && b->n_reqs * (long long)c->n_kv_heads >= 6LL * compute_units()) {
+  if (p.few && p.slices == 1 && steps <= 20 && b->n_reqs * (long long)c->n_kv_heads >= 6LL * compute_units()) {
     p.heads_log2 = 2;
     p.workgroups = b->n_reqs * ((c->n_kv_heads + 3LL) / 4);
   }
@@ -319,7 +343,8 @@ int sgmv_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t la
   a.q_starts = b->q_starts;
   a.kv_lens = b->kv_lens;
   a.tables = b->tables;
-  a.columns = plan.columns;
+  a.few = plan.few;
+  a.columns_log2 = plan.columns_log2;
   a.heads_log2 = plan.heads_log2;
   const long long covered = (long long)b->table_width * c->page_size, hint = b->max_kv_len > 0 && b->max_kv_len < covered ? b->max_kv_len : covered;
   a.classes = 8.0f / (float)(window > 0 && window < hint ? window : hint + 1);
@@ -350,7 +375,7 @@ int sgmv_plan_attention_q4(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32
   if (window < 0) return SGMV_ERR_SHAPE;
   if (nothing) return rc;
   const AttentionPlan p = plan_attention(c, b, n_heads, window, workspace == nullptr ? 0 : workspace_bytes);
-  plan->kernel = p.columns == kFewColumns ? SGMV_KERNEL_ATTENTION_FEW : SGMV_KERNEL_ATTENTION_MANY;
+  plan->kernel = p.few ? SGMV_KERNEL_ATTENTION_FEW : SGMV_KERNEL_ATTENTION_MANY;
   plan->launches = p.slices > 1 ? 2 : 1;
   plan->slices = p.slices;
   plan->workgroups = p.workgroups > INT32_MAX ? INT32_MAX : (int32_t)p.workgroups;

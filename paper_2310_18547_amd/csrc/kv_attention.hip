@@ -724,20 +724,20 @@ __device__ __forceinline__ bool tile_by_work(const AttentionArgs& a, int columns
   return true;
 }
 
-// 64 NT columns of one cache head.  grid = (cache heads x tiles, slices).
+// Up to 64 NT columns of one cache head (2^columns_log2; 2^7 where NT is 2).  grid = (cache heads x tiles, slices).
 template <class DT, int D, int NT>
 __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_many_kernel(AttentionArgs a, int first_tile, int tiles) {
-  constexpr int kLog2 = NT == 1 ? 6 : 7;
+  const int log2 = NT == 1 ? a.columns_log2 : 7;
   __shared__ Shared<D, NT> shared;
   __shared__ Ordered ordered;
   const int head = blockIdx.x % a.at.n_kv_heads, n = (int)(blockIdx.x / a.at.n_kv_heads), slice = blockIdx.y;
   Tile t;
   if (a.ordered) {
-    if (!tile_by_work(a, kLog2, 16 * NT, tiles, n, ordered, t)) return;
-  } else if (!tile_of_batch(a, kLog2, first_tile + tiles - 1 - n, t)) {
+    if (!tile_by_work(a, log2, 16 * NT, tiles, n, ordered, t)) return;
+  } else if (!tile_of_batch(a, log2, first_tile + tiles - 1 - n, t)) {
     return;
   }
-  const int columns = min(t.columns - t.first_column, 64 * NT);
+  const int columns = min(t.columns - t.first_column, 1 << log2);
   if (NT > 1 && columns <= 16)
     attend_tile<DT, D, 1, false, false>(a, t, columns, head, 0, slice, reinterpret_cast<Shared<D, 1>&>(shared));
   else
@@ -809,8 +809,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a, lo
 // Launches over ranges of tiles, fewer than 2^31 threads each.
 template <class F>
 hipError_t by_tiles(const AttentionArgs& a, F launch) {
-  const long long tiles = a.columns == kFewColumns ? a.n_reqs : attention_tiles(a.n_tokens, a.group, a.n_reqs, a.columns);
-  const int blocks = a.columns == kFewColumns ? (a.at.n_kv_heads + (1 << a.heads_log2) - 1) >> a.heads_log2 : a.at.n_kv_heads;
+  const long long tiles = a.few ? a.n_reqs : attention_tiles(a.n_tokens, a.group, a.n_reqs, 1 << a.columns_log2);
+  const int blocks = a.few ? (a.at.n_kv_heads + (1 << a.heads_log2) - 1) >> a.heads_log2 : a.at.n_kv_heads;
   // whole sixty-fours of requests
   const long long share = (1LL << 30) / 256 / a.slices / blocks & ~63LL, most = share > 0 ? share : 64;
   for (long long first = 0; first < tiles; first += most) {
@@ -827,14 +827,14 @@ hipError_t columns_typed(AttentionArgs a, hipStream_t st) {
   // In the order of their work where the launch goes through the chip a few times at most (eight prompts of up to 1024 rows, 32 heads, 1376 workgroups: 101 -> 86 us; two of
   // 4095 rows, 4104 workgroups: 848 -> 882); of one request the last tiles are the ones with most work anyway.
   a.ordered = a.n_reqs > 1 && a.n_reqs <= kMostOrdered;
-  const long long groups = attention_tiles(a.n_tokens, a.group, a.n_reqs, a.columns) * a.at.n_kv_heads * a.slices;
+  const long long groups = attention_tiles(a.n_tokens, a.group, a.n_reqs, 1 << a.columns_log2) * a.at.n_kv_heads * a.slices;
   a.ordered = a.ordered && groups > 2LL * compute_units() && groups <= 8LL * compute_units();
   return by_tiles(a, [&](dim3 grid, int first, int n) {
-    if (a.columns == kFewColumns && a.heads_log2 == 0)
+    if (a.few && a.heads_log2 == 0)
       attention_few_kernel<DT, D, 0><<<grid, 256, 0, st>>>(a, first);
-    else if (a.columns == kFewColumns)
+    else if (a.few)
       attention_few_kernel<DT, D, 2><<<grid, 256, 0, st>>>(a, first);
-    else if (a.columns == kSomeColumns)
+    else if (1 << a.columns_log2 < kManyColumns)
       attention_many_kernel<DT, D, 1><<<grid, 256, 0, st>>>(a, first, n);
     else
       attention_many_kernel<DT, D, 2><<<grid, 256, 0, st>>>(a, first, n);
