@@ -423,6 +423,18 @@ def test_attention_tiles_of_many_prompts(dtype, d, kv_heads, group, hint):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("requests,kv_heads,group,columns", [(1, 3, 2, 16), (8, 64, 1, 32), (8, 64, 2, 64), (8, 64, 5, 128)])
+def test_attention_tiles_of_every_width(dtype, d, requests, kv_heads, group, columns):
+    lens, new = [20 + 3 * (i % 5) for i in range(requests)], [20] * requests
+    cache = Cache(dtype, d, kv_heads, 1, 16, 4)
+    plan = plan_of(cache, lens, new, kv_heads * group, (20, max(lens)))
+    assert plan.kernel == sg.KERNEL_ATTENTION_MANY and plan.workgroups == (20 * requests * group // columns + requests) * kv_heads
+    check_attention(dtype, d, kv_heads * group, kv_heads, 16, lens, new, hints=(20, max(lens)), seed=columns)
+    check_attention(dtype, d, kv_heads * group, kv_heads, 16, lens, [20, 1, 0, 13, 20, 7, 20, 2][:requests], window=9, hints=(20, max(lens)), seed=columns)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("hints", [(40, 700), (40, 100000), (1000, 0)])
 def test_attention_of_prompts_in_slices(dtype, hints):
     """Rows behind long contexts, in slices; rows whose positions fit one slice are written by it, those without any by the join or not at all."""
