@@ -96,8 +96,8 @@ size_t slice_bytes(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int32_t n_hea
 // Time of an attention launch in us, to choose the kernel, the tiles and the slices by.
 //
 // Few columns: one, two and three workgroups to a unit take 1.2, 1.6 and 2.4 us for a step of 32 positions (the loads; 131 000 positions in 48, 64 and
-// 96 slices: 1.5, 1.8, 2.4), a workgroup's lookups, queries and end 4 us (64 requests of 512 to 2048 positions, 32 heads: 80 us whole, 133 in
-// six slices), and a batch's last round is half empty.
+// 96 slices: 1.5, 1.8, 2.4), a workgroup's lookups, queries and end 4 us (64 requests of 512 to 2048 positions, 32 heads, take two thirds more in
+// six slices than whole), and a batch's last round is half empty.
 // Tiles: 1.1 us a step and 4 us around them while tiles are few (1.15 and 6 where a wave has 32 columns), 1.4 (1.6) and 6.5 us where they queue
 // for units.  300 rows, 32 heads, in tiles of 16 / 32 / 64 / 128: 10 / 11 / 15 / 19 us; 600 and 600 rows 36 / 32 / 28 / 35; 8 prompts of up to 1024
 // 127 / 101 / 104 / 85; 453 rows next to 64 single tokens, 8 heads shared by 4 each, 36 / 30 / 26 / 32.
@@ -176,7 +176,8 @@ AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int
     }
   }
   // A wave to a head saves its waves' common start and end where there are heads enough and all contexts are short (64 requests of 32 heads, a head to a
-  // workgroup / to a wave: 128 positions 21.9 / 12.9 us, 512 40.7 / 33.4, 1024 63.7 / 58.3; but 512 to 2048 81 / 91, where the longest are left running).
+  // workgroup / to a wave: 128 positions 20.7 / 13.1 us, 512 37.2 / 31.8, 768 47.4 / 44.2; but 100 to 1000 39 / 45, 512 to 2048 73 / 87, where the
+  // longest are left running).
   if (p.few && p.slices == 1 && steps <= 20 && b->n_reqs * (long long)c->n_kv_heads >= 6LL * compute_units()) {
     p.heads_log2 = 2;
     p.workgroups = b->n_reqs * ((c->n_kv_heads + 3LL) / 4);
