@@ -398,9 +398,24 @@ __device__ __forceinline__ void score_step(const Held<D>& s, int first_pos, uint
   for (int n = 0; n < NT; ++n) r.above |= r.highest[n] > c.bar[n];
 }
 
+// v's codes of two positions side by side, halves of their words; odd positions from the top down.
+template <int D>
+struct Beside {
+  uint32_t codes[D / 64][4];
+};
+template <int D>
+__device__ __forceinline__ void put_beside(const Held<D>& s, int lane, Beside<D>& b) {
+  const uint32_t pairs[4][2] = {{s.v[0].x, ~s.v[0].y}, {s.v[0].z, ~s.v[0].w}, {s.v[1].x, ~s.v[1].y}, {s.v[1].z, ~s.v[1].w}};
+  const uint32_t own = D == 128 || (lane & 8) == 0 ? 0x05040100u : 0x07060302u;
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b.codes[h][e] = __builtin_amdgcn_perm(pairs[e][1], pairs[e][0], h == 0 ? own : 0x07060302u);
+}
+
 // Weights of a step and the weighted values.
 template <class DT, int D, int NT, bool MASKED>
-__device__ __forceinline__ void weigh_step(const Held<D>& s, int lane, Scores<NT>& r, Columns<D, NT>& c) {
+__device__ __forceinline__ void weigh_step(const Beside<D>& v, Scores<NT>& r, Columns<D, NT>& c) {
   constexpr bool kTwoParts = std::is_same_v<DT, F16>;
   uint32_t high[NT][4], rest[NT][4];
   auto weigh = [&](auto which) {
@@ -428,14 +443,12 @@ __device__ __forceinline__ void weigh_step(const Held<D>& s, int lane, Scores<NT
   weigh(std::integral_constant<int, 6>{}), weigh(std::integral_constant<int, 7>{});
 
   // v's codes as first operands of out^T = V^T w^T: row i of output tile j is value 8 i + j of a head of 128, 8 (i % 8) + 4 (i / 8) + j of
-  // one of 64; halves of the words of two positions side by side
-  const uint32_t pairs[4][2] = {{s.v[0].x, ~s.v[0].y}, {s.v[0].z, ~s.v[0].w}, {s.v[1].x, ~s.v[1].y}, {s.v[1].z, ~s.v[1].w}};
-  const uint32_t own = D == 128 || (lane & 8) == 0 ? 0x05040100u : 0x07060302u;
+  // one of 64
 #pragma unroll
   for (int h = 0; h < D / 64; ++h) {
     uint4 parts[4];  // of a pair of positions each: tiles 4 h .. 4 h + 3
 #pragma unroll
-    for (int e = 0; e < 4; ++e) parts[e] = unpack_codes(__builtin_amdgcn_perm(pairs[e][1], pairs[e][0], h == 0 ? own : 0x07060302u));
+    for (int e = 0; e < 4; ++e) parts[e] = unpack_codes(v.codes[h][e]);
     const uint4 codes[4] = {make_uint4(parts[0].x, parts[1].x, parts[2].x, parts[3].x), make_uint4(parts[0].y, parts[1].y, parts[2].y, parts[3].y),
                             make_uint4(parts[0].z, parts[1].z, parts[2].z, parts[3].z), make_uint4(parts[0].w, parts[1].w, parts[2].w, parts[3].w)};
 #pragma unroll
@@ -452,7 +465,8 @@ __device__ __forceinline__ void weigh_step(const Held<D>& s, int lane, Scores<NT
   }
 }
 
-// The next step's keys are loaded as soon as the scores are there, its values after the products with this one's.
+// The next step's keys and values are loaded as soon as the scores are there and the values' words put beside one another, a whole step of weights ahead: the
+// compiler left to itself moves them behind it (2 to 9 % slower).
 template <class DT, int D, int NT, bool ONCE>
 __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages& p, int begin, int end, int stride_log2, int lane, Columns<D, NT>& c) {
   if (begin >= end) return;
@@ -483,12 +497,18 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
     pages = look_up(a, p, step_at(n + 2));
   };
   Scores<NT> r;
+  Beside<D> beside;
+  auto ahead = [&] {
+    put_beside<D>(held, lane, beside);
+    load_k<D, ONCE>(next, offsets, held);
+    load_v<D, ONCE>(next, offsets, held);
+    __builtin_amdgcn_sched_barrier(0);
+  };
   while (n < ends) {
     score_step<DT, D, NT, true>(held, step_at(n) * kStepPositions, at.there, lane, c, r);
-    load_k<D, ONCE>(next, offsets, held);
+    ahead();
     if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
-    weigh_step<DT, D, NT, true>(held, lane, r, c);
-    load_v<D, ONCE>(next, offsets, held);
+    weigh_step<DT, D, NT, true>(beside, r, c);
     on();
   }
   while (n < count) {
@@ -496,9 +516,8 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
     score_step<DT, D, NT, false>(held, 0, at.there, lane, c, r);
     if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
     for (;;) {
-      load_k<D, ONCE>(next, offsets, held);
-      weigh_step<DT, D, NT, false>(held, lane, r, c);
-      load_v<D, ONCE>(next, offsets, held);
+      ahead();
+      weigh_step<DT, D, NT, false>(beside, r, c);
       on();
       if (n >= count) break;
       score_step<DT, D, NT, false>(held, 0, at.there, lane, c, r);
