@@ -177,7 +177,7 @@ AttentionPlan plan_attention(const sgmv_kv_cache* c, const sgmv_kv_batch* b, int
   }
   // A wave to a head saves its waves' common start and end where there are heads enough and all contexts are short (64 requests of 32 heads, a head to a
   // workgroup / to a wave: 128 positions 20.7 / 13.1 us, 512 37.2 / 31.8, 768 47.4 / 44.2; but 100 to 1000 39 / 45, 512 to 2048 73 / 87, where the
-  // longest are left running).
+  // longest are left running; all some 5 % less since).
   if (p.few && p.slices == 1 && steps <= 20 && b->n_reqs * (long long)c->n_kv_heads >= 6LL * compute_units()) {
     p.heads_log2 = 2;
     p.workgroups = b->n_reqs * ((c->n_kv_heads + 3LL) / 4);

@@ -745,9 +745,9 @@ __device__ __forceinline__ bool tile_by_work(const AttentionArgs& a, int columns
 
 // Up to 64 NT columns of one cache head (2^columns_log2; 2^7 where NT is 2).  grid = (cache heads x tiles, slices).
 //
-// Bound by the vector units, busy for 80 % of the time of two prompts of 4095 rows (the matrix cores for 28 %): a step of 32 positions takes a wave with 32
+// Bound by the vector units, busy for 82 % of the time of two prompts of 4095 rows (the matrix cores for 29 %): a step of 32 positions takes a wave with 32
 // columns some 320 instructions besides its 32 products, 126 of them for the codes of k and v whatever its columns.  8000 rows of 32 heads, 8 of the
-// cache, bfloat16 735 us (714 TFLOP/s), binary16, whose weights are two parts, 855; those two prompts, 64 heads, 8 of the cache, 856.  Four tiles of sixteen
+// cache, bfloat16 706 us (743 TFLOP/s), binary16, whose weights are two parts, 828; those two prompts, 64 heads, 8 of the cache, 826.  Four tiles of sixteen
 // columns to a wave would halve the codes' part: their 256 registers and more to a lane leave one wave to a SIMD, 2100 us.  Codes unpacked once for the
 // four waves, through LDS: a quarter fewer instructions, 877 us where this took 848, for a barrier a step.
 template <class DT, int D, int NT>
@@ -772,8 +772,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_many_kernel(At
 // Requests of up to sixteen columns (more than the hint said: sixteen after sixteen), 2^HEADS_LOG2 cache heads to a workgroup.
 // grid = (cache heads / that x requests, slices).
 //
-// Bound by memory: 64 requests of 2048 positions, 32 heads, 571 MB, 103 us (5.5 TB/s; a read of 1 GiB reaches 5.9), of 512 to 2048 73 us (5.2; the last long
-// ones are alone), of 512 31.8; one of 130 000 positions, 8 heads, in 64 slices 29 us and 5 for their join.  Three waves to a SIMD: four (128 registers)
+// Bound by memory: 64 requests of 2048 positions, 32 heads, 571 MB, 98 us (5.9 TB/s, as a read of 1 GiB), of 512 to 2048 72.5 us (5.2; the last long ones are
+// alone), of 512 28.7; one of 130 000 positions, 8 heads, in 64 slices 29 us and 5 for their join.  Three waves to a SIMD: four (128 registers)
 // spill, two with two steps held at once are 3 % slower.
 template <class DT, int D, int HEADS_LOG2>
 __global__ __launch_bounds__(256, 3) void attention_few_kernel(AttentionArgs a, int first_request) {
