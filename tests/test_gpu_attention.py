@@ -705,6 +705,35 @@ def test_pages_far_apart():
     assert all(torch.equal(a, b) for a, b in zip(*results)) and bool(results[0][0].abs().sum() > 0)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("hint", [1, 30])
+def test_attention_of_seventy_thousand_requests(dtype, hint):
+    """A position each, so that every result is its row of v; every third request has no row."""
+    n, d, heads = 70001, 64, 2
+    cache = Cache(dtype, d, 1, 2, 16, n)
+    tables = torch.randperm(n, device="cuda", dtype=torch.int32)[:, None].contiguous()
+    slots = (tables[:, 0] * 16).contiguous()
+    k, v = (torch.randn(n, d, device="cuda").to(KIND[dtype]) for _ in range(2))
+    sg.sgmv_kv_append_q4(cache.c, sg.make_kv_batch(n, n, 1, None, None, None, slots), 1, None, None, k, v, heads, heads * d, heads * d, d)
+    held = torch.zeros_like(v)
+    sg.sgmv_kv_read_q4(cache.c, 1, None, held, d, slots, n)
+    has = torch.arange(n, device="cuda") % 3 != 2
+    starts = torch.cat((torch.zeros(1, dtype=torch.int64, device="cuda"), has.cumsum(0))).int()
+    rows = int(starts[-1])
+    q = torch.randn(rows, heads * d, device="cuda").to(KIND[dtype])
+    out = torch.zeros_like(q)
+    lens = torch.ones(n, dtype=torch.int32, device="cuda")
+    b = sg.make_kv_batch(n, rows, 1, starts, lens, tables, max_q_len=hint, max_kv_len=1)
+    assert sg.sgmv_plan_attention_q4(cache.c, b, heads).kernel == (sg.KERNEL_ATTENTION_FEW if hint == 1 else sg.KERNEL_ATTENTION_MANY)
+    sg.sgmv_attention_q4(cache.c, b, 1, out, None, q, heads, heads * d, heads * d, 0.125)
+    want = held[has][:, None].double()
+    # the row is rounded once there, and here once after products and sums of fp32 (of the code, weighted, and the minimum: 2^-11 of the larger
+    # part in bfloat16, whose weights have 11 bits)
+    off = (out.view(rows, heads, d).double() - want).abs()
+    spread = held[has].double().abs().amax(-1)[:, None, None]
+    assert bool((off <= 2 * ref.HALF_STEP[dtype] * want.abs() + spread * (4 * ref.WEIGHT_STEP[dtype] + 2.0 ** -20)).all())
+
+
 def test_a_served_batch_step_after_step():
     """assign, append and attend together: two prompts, then single tokens, one request over and another in its place."""
     rng = np.random.default_rng(13)
