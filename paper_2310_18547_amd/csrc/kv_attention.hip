@@ -315,10 +315,13 @@ __device__ __forceinline__ void raise(Columns<D, NT>& c, const float (&highest)[
     float top = fmaxf(highest[n], __shfl_xor(highest[n], 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     top = fmaxf(top, c.top[n]);
-    const float shrink = __builtin_amdgcn_exp2f((c.top[n] - top) * c.q[n].factor) * by;
+    // A column that has seen nothing yet stays as it began, whatever its neighbours raise: the first score that it sees has to raise it (kBehind
+    // of a factor of 2^-126 would put the bar above any), and kLowest times the factor is no base to subtract from the score of a hidden page.
+    const bool blind = top == kLowest;
+    const float shrink = blind ? 1.0f : __builtin_amdgcn_exp2f((c.top[n] - top) * c.q[n].factor) * by;
     c.top[n] = top;
-    c.bar[n] = top + kBehind / c.q[n].factor;
-    c.base[n] = fmaf(top, c.q[n].factor, -(float)unit);
+    c.bar[n] = blind ? kLowest : top + kBehind / c.q[n].factor;
+    c.base[n] = blind ? 0.0f : fmaf(top, c.q[n].factor, -(float)unit);
     c.sum[n] *= shrink;
     c.minima[n] *= shrink;
 #pragma unroll
@@ -626,7 +629,7 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float sum = of_column(c.sum[n]), minima = of_column(c.minima[n]);
-      const float base = c.top[n] == kLowest ? kLowest : c.base[n];
+      const float base = sum == 0.0f ? kLowest : c.base[n];
       const int column = first + n * 16 + i;
       if (column >= t.columns) continue;
       const int row = column / a.group, q_head = head * a.group + column - row * a.group;

@@ -1,0 +1,64 @@
+"""Attention over the paged 4-bit cache where a column has seen nothing yet, sees nothing at all, or sees what lies far apart."""
+import numpy as np
+import pytest
+import torch
+
+import attention_reference as ref
+import paper_2310_18547_amd as sg
+from backbone_reference import round16
+from helpers import decode64
+from test_gpu_attention import attend, bits16, check_attention, filled_cache, host, host16, normal, rows_of
+
+pytestmark = pytest.mark.gpu
+
+
+def slices_of(cache, tables, n_tokens, heads, hints, scratch, window=0):
+    b = sg.make_kv_batch(len(tables), n_tokens, tables.shape[1], None, None, None, max_q_len=hints[0], max_kv_len=hints[1])
+    return sg.sgmv_plan_attention_q4(cache.c, b, heads, window, 1 << 8 if scratch else None, scratch).slices
+
+
+def plan_slices(dtype, d, heads, kv_heads, page, lens, new, hints, scratch, window=0, tail=2):
+    """Slices of check_attention's call of these shapes."""
+    held = [-(-n // page) for n in lens]
+    c = sg.make_kv_cache(sg.F16 if dtype == "f16" else sg.BF16, d, kv_heads, 2, page, sum(held) + 2)
+    b = sg.make_kv_batch(len(lens), sum(new) + tail, max(held) + 1, None, None, None, max_q_len=hints[0], max_kv_len=hints[1])
+    return sg.sgmv_plan_attention_q4(c, b, heads, window, 1 << 8 if scratch else None, scratch).slices
+
+
+# ---------------------------------------------------------------------------------------------- columns that have seen nothing yet
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,kv_heads,new", [(2, 2, 4), (4, 2, 4), (3, 1, 40)])
+@pytest.mark.parametrize("window", [0, 150])
+def test_zero_queries_whose_wave_begins_with_a_step_that_they_do_not_see(dtype, heads, kv_heads, new, window):
+    """A wave takes the step that a mask cuts first, and its first rows see nothing there: their first score must still count, with scores of 0
+    and a scale so small that the distance by which a maximum may lag is not finite."""
+    for scale in (1 / 128, 1 / 512, 1e-30):
+        check_attention(dtype, 128, heads, kv_heads, 16, [194], [new], window=window, q_size=0.0, scale=scale, seed=1)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("window", [0, 3000])
+def test_zero_queries_in_slices(dtype, window):
+    for lens in ([4002], [4097], [4030]):
+        hints, scratch = (4, lens[0]), 1 << 22
+        assert plan_slices(dtype, 128, 2, 2, 16, lens, [4], hints, scratch, window) > 1
+        check_attention(dtype, 128, 2, 2, 16, lens, [4], window=window, q_size=0.0, scale=1 / 128, scratch=scratch, hints=hints, seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,new", [(2, 4), (6, 30)])
+@pytest.mark.parametrize("gone", [(0, 1), (2, 3, 4, 5), (0, 1, 4, 5, 8)])
+def test_hidden_pages_behind_a_step_that_a_row_does_not_see(dtype, heads, new, gone):
+    """The first step that a column sees whole lies on pages that are not of the cache, after its neighbours have raised their maxima."""
+    rng = np.random.default_rng(len(gone))
+    for n in (130, 131, 162):
+        cache, pages, tables = filled_cache(rng, dtype, 128, 2, 16, [n])
+        tables[0, list(gone)] = -1
+        q = normal(rng, (new, heads, 128), dtype)
+        out, lse = attend(cache, tables, [0, new], [n], bits16(q.reshape(new, -1), dtype), heads, 0.088)
+        hidden = lambda r: np.isin(np.arange(n) // 16, gone)  # noqa: E731
+        want, want_lse, off, spread = ref.attention(decode64(q, dtype), rows_of(pages, tables, 16), [0, new], [n], heads, 2, 0.088, hidden=hidden)
+        got = decode64(host16(out), dtype).reshape(want.shape)
+        assert (np.abs(got - want) <= ref.tolerance(want, off, spread, dtype)).all(), n
+        assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
