@@ -628,7 +628,9 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
     attend_steps<DT, D, NT, ONCE>(a, p, steps.begin + (wave >> groups_log2), steps.end, 2 - groups_log2, lane, c);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float sum = of_column(c.sum[n]), minima = of_column(c.minima[n]);
+      // a query without a factor (see load_query): by what is its to see, not by what its steps' products made of it
+      const float sum = isnan(c.q[n].factor) ? (c.span[n].high > c.span[n].low ? c.q[n].factor : 0.0f) : of_column(c.sum[n]);
+      const float minima = of_column(c.minima[n]);
       const float base = sum == 0.0f ? kLowest : c.base[n];
       const int column = first + n * 16 + i;
       if (column >= t.columns) continue;

@@ -62,3 +62,51 @@ def test_hidden_pages_behind_a_step_that_a_row_does_not_see(dtype, heads, new, g
         got = decode64(host16(out), dtype).reshape(want.shape)
         assert (np.abs(got - want) <= ref.tolerance(want, off, spread, dtype)).all(), n
         assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
+
+
+# ---------------------------------------------------------------------------------------------- rows that see nothing
+
+@pytest.mark.parametrize("dtype,bad", [("f16", 0x7FFF), ("f16", 0x7C00), ("bf16", 0x7FFF), ("bf16", 0x7F80), ("bf16", 0x7200)])  # the last: 2^101
+@pytest.mark.parametrize("heads", [2, 6])
+@pytest.mark.parametrize("hints", [(0, 0), (2, 0)])
+def test_queries_that_are_not_finite_and_see_nothing(dtype, bad, heads, hints):
+    """Rows in front of position 0 are zeros with a sum of nothing, whatever they hold and whoever shares their tile."""
+    rng = np.random.default_rng(3)
+    lens, new = [3, 0, 40], [9, 4, 42]
+    cache, pages, tables = filled_cache(rng, dtype, 128, 2, 16, lens)
+    starts = np.concatenate(([0], np.cumsum(new)))
+    q = normal(rng, (55, heads, 128), dtype)
+    rows = [1, 7, 10, 14, 30]  # of the first request one in front of position 0 and one that sees positions, of the second, of the third as the first
+    for row in rows:
+        q[row, :, 5] = bad
+    out, lse = attend(cache, tables, starts, lens, bits16(q.reshape(55, -1), dtype), heads, 0.088, hints=hints)
+    got, sums = decode64(host16(out), dtype).reshape(55, heads, 128), host(lse)
+    blind = np.r_[0:6, 9:13, 13:15]
+    assert (got[blind] == 0).all() and np.isneginf(sums[blind]).all()
+    for row in (7, 30):
+        assert np.isnan(got[row]).all() and np.isnan(sums[row]).all()
+    clean = q.copy()
+    clean[rows] = 0
+    want, want_lse, off, spread = ref.attention(decode64(clean, dtype), rows_of(pages, tables, 16), starts, lens, heads, 2, 0.088)
+    fine = np.setdiff1d(np.arange(55), (7, 30))
+    assert (np.abs(got - want)[fine] <= ref.tolerance(want, off, spread, dtype)[fine]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [20, 32, 40, 300, 4000])
+def test_queries_that_are_not_finite_over_hidden_pages(dtype, n):
+    """NaN where positions are theirs to see, on pages of the cache or not; the others see nothing."""
+    rng = np.random.default_rng(4)
+    cache, pages, tables = filled_cache(rng, dtype, 64, 1, 16, [n])
+    tables[:] = -1
+    q = normal(rng, (3, 2, 64), dtype)
+    q[1, 0, 3] = 0x7FFF
+    hints, scratch = (3, n), 1 << 22
+    assert n < 4000 or slices_of(cache, tables, 3, 2, hints, scratch) > 1
+    for causal in (0, 1):
+        out, lse = attend(cache, tables, [0, 3], [n], bits16(q.reshape(3, -1), dtype), 2, 0.125, causal, scratch=scratch, hints=hints)
+        got, sums = decode64(host16(out), dtype).reshape(3, 2, 64), host(lse)
+        bad = np.zeros((3, 2), bool)
+        bad[1, 0] = True
+        assert np.isnan(got[bad]).all() and np.isnan(sums[bad]).all()
+        assert (got[~bad] == 0).all() and np.isneginf(sums[~bad]).all()
