@@ -33,6 +33,12 @@ constexpr float kLowest = -3.0e38f;
 constexpr int kWeightTop = 11, kMostUnit = 90;
 constexpr float kMinimum = 0x1p-60f;
 constexpr float kBehind = 4.0f;
+// Maxima beyond it (in powers of two) are taken off the scores themselves: as part of a base they would be rounded, by 2^-8 here, by 2^7 at
+// scores of 2^31, which rows of binary16 have, and a weight of 1 would be worth nothing, or no number.  Such a column goes through raise() at every
+// step, so that the others' steps know nothing of it (a branch in them took 4 %).
+constexpr float kFar = 0x1p16f;
+// What a weight of 1 is worth in parts of such a column, in powers of two: base and unit apart, they would not meet as equals.
+constexpr int kFarUnit = -20;
 
 // Codes of a word's halves as binary16 operands of 2^-20 each: values n and n + 4 of part n.
 __device__ __forceinline__ uint4 unpack_codes(uint32_t w) {
@@ -279,7 +285,7 @@ struct Columns {
   Span some, all;    // positions that some column of the wave sees, and that all do
   float top[NT];     // maximum of the scores, up to kBehind of it behind, the same in all lanes of a column
   float bar[NT];     // scores above it raise the maximum
-  float base[NT];    // 2^base: what a weight of 1 is worth
+  float base[NT];    // 2^base: what a weight of 1 is worth (next to the maximum, where that is far)
   float sum[NT];     // of the weights
   float minima[NT];  // of the weights times v's minima
   f32x4 acc[NT][D / 16];  // of the weights times v's codes and scales, times 2^-20
@@ -299,10 +305,23 @@ __device__ __forceinline__ void start_columns(Columns<D, NT>& c, int lane) {
   c.limit = lane & 8 ? 0.0f : __uint_as_float(0x7F800000u);
 }
 
-// Raises the columns' maxima to those of this step's scores and lowers the unit to its scales.
+// What a step's scores are, and the scales and minima of its positions (a lane's own, see Held).
+template <int NT>
+struct Scores {
+  float x[NT][8], highest[NT];
+  uint32_t sees[NT];  // a bit for every position that the column sees
+  float scale, low, size;  // size: what the weights are to fit
+  bool above;         // of a bar or a limit: raise() is due
+};
 template <int D, int NT>
-__device__ __forceinline__ void raise(Columns<D, NT>& c, const float (&highest)[NT], float scale, int lane) {
-  float s = lane & 8 ? scale : 0.0f;
+__device__ __forceinline__ bool is_far(const Columns<D, NT>& c, int n) {
+  return fabsf(c.top[n] * c.q[n].factor) > kFar;
+}
+
+// Raises the columns' maxima to those of this step's scores and lowers the unit to its scales; takes maxima that are far off the scores.
+template <int D, int NT>
+__device__ __forceinline__ void raise(Columns<D, NT>& c, Scores<NT>& r, int lane) {
+  float s = lane & 8 ? r.size : 0.0f;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) s = fmaxf(s, __shfl_xor(s, m));
   const int fits = min(kWeightTop - ((int)(__float_as_uint(s) >> 23) - 126), kMostUnit);  // s < 2^(kWeightTop - fits)
@@ -312,7 +331,7 @@ __device__ __forceinline__ void raise(Columns<D, NT>& c, const float (&highest)[
   if (lane & 8) c.limit = ldexpf(1.0f, kWeightTop - unit);
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    float top = fmaxf(highest[n], __shfl_xor(highest[n], 16));
+    float top = fmaxf(r.highest[n], __shfl_xor(r.highest[n], 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     top = fmaxf(top, c.top[n]);
     // A column that has seen nothing yet stays as it began, whatever its neighbours raise: the first score that it sees has to raise it (kBehind
@@ -320,8 +339,13 @@ __device__ __forceinline__ void raise(Columns<D, NT>& c, const float (&highest)[
     const bool blind = top == kLowest;
     const float shrink = blind ? 1.0f : __builtin_amdgcn_exp2f((c.top[n] - top) * c.q[n].factor) * by;
     c.top[n] = top;
-    c.bar[n] = blind ? kLowest : top + kBehind / c.q[n].factor;
-    c.base[n] = blind ? 0.0f : fmaf(top, c.q[n].factor, -(float)unit);
+    const bool far = !blind && is_far(c, n);
+    c.bar[n] = blind ? kLowest : far ? -__uint_as_float(0x7F800000u) : top + kBehind / c.q[n].factor;
+    c.base[n] = blind ? 0.0f : fmaf(far ? 0.0f : top, c.q[n].factor, -(float)unit);
+    if (__any(far)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r.x[n][e] -= far ? top : 0.0f;
+    }
     c.sum[n] *= shrink;
     c.minima[n] *= shrink;
 #pragma unroll
@@ -329,14 +353,6 @@ __device__ __forceinline__ void raise(Columns<D, NT>& c, const float (&highest)[
   }
 }
 
-// What a step's scores are, and the scales and minima of its positions (a lane's own, see Held).
-template <int NT>
-struct Scores {
-  float x[NT][8], highest[NT];
-  uint32_t sees[NT];  // a bit for every position that the column sees
-  float scale, low, size;  // size: what the weights are to fit
-  bool above;         // of a bar or a limit: raise() is due
-};
 // Scores of the 32 positions whose keys are in `s`.  MASKED: some column does not see all of them, or a tile is not `there`.
 template <class DT, int D, int NT, bool MASKED>
 __device__ __forceinline__ void score_step(const Held<D>& s, int first_pos, uint32_t there, int lane, const Columns<D, NT>& c, Scores<NT>& r) {
@@ -510,14 +526,14 @@ __device__ __forceinline__ void attend_steps(const AttentionArgs& a, const Pages
   while (n < ends) {
     score_step<DT, D, NT, true>(held, step_at(n) * kStepPositions, at.there, lane, c, r);
     ahead();
-    if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
+    if (__any(r.above)) raise<D, NT>(c, r, lane);
     weigh_step<DT, D, NT, true>(beside, r, c);
     on();
   }
   while (n < count) {
     // raise() stands outside of the inner loop, and the step is begun again for it: inside, the sums would be copied at every step
     score_step<DT, D, NT, false>(held, 0, at.there, lane, c, r);
-    if (__any(r.above)) raise<D, NT>(c, r.highest, r.size, lane);
+    if (__any(r.above)) raise<D, NT>(c, r, lane);
     for (;;) {
       ahead();
       weigh_step<DT, D, NT, false>(beside, r, c);
@@ -629,9 +645,11 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       // a query without a factor (see load_query): by what is its to see, not by what its steps' products made of it
-      const float sum = isnan(c.q[n].factor) ? (c.span[n].high > c.span[n].low ? c.q[n].factor : 0.0f) : of_column(c.sum[n]);
-      const float minima = of_column(c.minima[n]);
-      const float base = sum == 0.0f ? kLowest : c.base[n];
+      const bool far = is_far(c, n);
+      const float worth = far ? ldexpf(1.0f, kFarUnit - c.unit) : 1.0f;
+      const float sum = isnan(c.q[n].factor) ? (c.span[n].high > c.span[n].low ? c.q[n].factor : 0.0f) : of_column(c.sum[n]) * worth;
+      const float minima = of_column(c.minima[n]) * worth;
+      const float base = sum == 0.0f ? kLowest : far ? fmaf(c.top[n], c.q[n].factor, -(float)kFarUnit) : c.base[n];
       const int column = first + n * 16 + i;
       if (column >= t.columns) continue;
       const int row = column / a.group, q_head = head * a.group + column - row * a.group;
@@ -640,7 +658,7 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
         const int value = value_of<D>(4 * g + r);
         float v[D / 16];
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) v[j] = c.acc[n][j][r] * 0x1p20f;
+        for (int j = 0; j < D / 16; ++j) v[j] = c.acc[n][j][r] * (worth * 0x1p20f);
         if (groups_log2 < 2) {
 #pragma unroll
           for (int j = 0; j < D / 16; ++j) shared.sums[wave][n * 16 + i][value + j] = v[j];

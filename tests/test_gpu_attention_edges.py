@@ -110,3 +110,60 @@ def test_queries_that_are_not_finite_over_hidden_pages(dtype, n):
         bad[1, 0] = True
         assert np.isnan(got[bad]).all() and np.isnan(sums[bad]).all()
         assert (got[~bad] == 0).all() and np.isneginf(sums[~bad]).all()
+
+
+# ---------------------------------------------------------------------------------------------- scores and values far apart
+
+FAR = [("f16", 200.0, 200.0, 0.088), ("f16", 3000.0, 3000.0, 0.088), ("f16", 3e4, 3e4, 0.088), ("bf16", 300.0, 1000.0, 0.088), ("bf16", 1e5, 1e5, 0.088),
+       ("bf16", 2.0 ** 40, 2.0 ** 40, 1.0), ("bf16", 2.0 ** 50, 2.0 ** 49, 1.0), ("bf16", 2.0 ** -60, 2.0 ** -40, 2.0 ** 126)]
+
+
+def far_case(rng, dtype, size, n, keys):
+    """A cache of ``n`` positions whose keys are those of ``keys(k)``, made from one row of +-size and values of its own."""
+    cache, pages, tables = filled_cache(rng, dtype, 128, 1, 16, [n])
+    row = round16((size * rng.choice((-1.0, 1.0), 128)).astype(np.float32), dtype)
+    k = keys(np.broadcast_to(row, (n, 1, 128)).copy())
+    p = np.arange(n)
+    pages.write(1, tables[0, p // 16] * 16 + p % 16, k, normal(rng, (n, 1, 128), dtype))
+    cache.put(pages)
+    return cache, pages, tables, row
+
+
+@pytest.mark.parametrize("dtype,q_size,k_size,scale", FAR)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("n,scratch", [(20, 0), (300, 0), (2500, 1 << 22)])
+def test_large_scores_that_are_all_alike(dtype, q_size, k_size, scale, sign, n, scratch):
+    """Equal keys: every position weighs the same, however large the score (up to 2^107 here)."""
+    rng = np.random.default_rng(5)
+    cache, pages, tables, row = far_case(rng, dtype, k_size, n, lambda k: k)
+    q = round16(np.broadcast_to((sign * q_size * np.sign(decode64(row, dtype))).astype(np.float32), (1, 2, 128)), dtype)
+    hints = (1, n)
+    assert not scratch or slices_of(cache, tables, 1, 2, hints, scratch) > 1
+    out, lse = attend(cache, tables, [0, 1], [n], bits16(q.reshape(1, -1), dtype), 2, scale, scratch=scratch, hints=hints)
+    want, want_lse, off, spread = ref.attention(decode64(q, dtype), rows_of(pages, tables, 16), [0, 1], [n], 2, 1, scale)
+    assert np.abs(want_lse).max() > 100
+    got = decode64(host16(out), dtype).reshape(want.shape)
+    # scores of the same bytes are the same to the bit: the sum of the weights alone is rounded
+    alike = np.full_like(off, (n + 16) * 2.0 ** -24)
+    assert (np.abs(got - want) <= ref.tolerance(want, alike, spread, dtype)).all()
+    assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
+
+
+@pytest.mark.parametrize("dtype,q_size,k_size,scale", FAR)
+@pytest.mark.parametrize("n,scratch", [(300, 0), (2500, 1 << 22)])
+def test_large_scores_of_which_one_is_the_largest(dtype, q_size, k_size, scale, n, scratch):
+    """All keys point away but one, wherever that stands: the result is its value."""
+    rng = np.random.default_rng(6)
+    for at in (0, 37, n // 2, n - 1):
+        def keys(k):
+            k[np.arange(n) != at] ^= 0x8000
+            return k
+        cache, pages, tables, row = far_case(rng, dtype, k_size, n, keys)
+        q = round16(np.broadcast_to((q_size * np.sign(decode64(row, dtype))).astype(np.float32), (1, 2, 128)), dtype)
+        hints = (1, n)
+        out, lse = attend(cache, tables, [0, 1], [n], bits16(q.reshape(1, -1), dtype), 2, scale, scratch=scratch, hints=hints)
+        want, want_lse, off, spread = ref.attention(decode64(q, dtype), rows_of(pages, tables, 16), [0, 1], [n], 2, 1, scale)
+        got = decode64(host16(out), dtype).reshape(want.shape)
+        # the other weights are nothing in any precision (e^-200 and less)
+        assert (np.abs(got - want) <= ref.tolerance(want, np.full_like(off, 16 * 2.0 ** -24), spread, dtype)).all(), at
+        assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
