@@ -37,8 +37,11 @@ constexpr float kBehind = 4.0f;
 // scores of 2^31, which rows of binary16 have, and a weight of 1 would be worth nothing, or no number.  Such a column goes through raise() at every
 // step, so that the others' steps know nothing of it (a branch in them took 4 %).
 constexpr float kFar = 0x1p16f;
-// What a weight of 1 is worth in parts of such a column, in powers of two: base and unit apart, they would not meet as equals.
-constexpr int kFarUnit = -20;
+// What a weight of 1 is worth at least, in powers of two, where parts of a column meet, and exactly in those of a far one, which would not meet as
+// equals with units of their own.  From here to kMostUnit fp32 holds the sums of both; a unit is as low as -114 next to the largest scales.
+constexpr int kLeastUnit = -20;
+// What a sum is multiplied by in one go, of as many powers of two as a unit may fall by at once.
+constexpr int kMostFall = 100;
 
 // Codes of a word's halves as binary16 operands of 2^-20 each: values n and n + 4 of part n.
 __device__ __forceinline__ uint4 unpack_codes(uint32_t w) {
@@ -326,7 +329,8 @@ __device__ __forceinline__ void raise(Columns<D, NT>& c, Scores<NT>& r, int lane
   for (int m = 1; m < 64; m <<= 1) s = fmaxf(s, __shfl_xor(s, m));
   const int fits = min(kWeightTop - ((int)(__float_as_uint(s) >> 23) - 126), kMostUnit);  // s < 2^(kWeightTop - fits)
   const int unit = min(c.unit, fits);
-  const float by = ldexpf(1.0f, unit - c.unit);
+  const int fall = c.unit - unit;
+  const float by = ldexpf(1.0f, -min(fall, kMostFall));
   c.unit = unit;
   if (lane & 8) c.limit = ldexpf(1.0f, kWeightTop - unit);
 #pragma unroll
@@ -350,6 +354,16 @@ __device__ __forceinline__ void raise(Columns<D, NT>& c, Scores<NT>& r, int lane
     c.minima[n] *= shrink;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) c.acc[n][j] *= shrink;
+  }
+  if (__any(fall > kMostFall)) {  // from values of nothing to 2^20 and more: what is left of the power of two would be 0 as one factor
+    const float rest = ldexpf(1.0f, kMostFall - fall);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      c.sum[n] *= rest;
+      c.minima[n] *= rest;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) c.acc[n][j] *= rest;
+    }
   }
 }
 
@@ -645,11 +659,11 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       // a query without a factor (see load_query): by what is its to see, not by what its steps' products made of it
-      const bool far = is_far(c, n);
-      const float worth = far ? ldexpf(1.0f, kFarUnit - c.unit) : 1.0f;
+      const bool moved = c.unit < kLeastUnit || is_far(c, n);
+      const float worth = moved ? ldexpf(1.0f, kLeastUnit - c.unit) : 1.0f;
       const float sum = isnan(c.q[n].factor) ? (c.span[n].high > c.span[n].low ? c.q[n].factor : 0.0f) : of_column(c.sum[n]) * worth;
       const float minima = of_column(c.minima[n]) * worth;
-      const float base = sum == 0.0f ? kLowest : far ? fmaf(c.top[n], c.q[n].factor, -(float)kFarUnit) : c.base[n];
+      const float base = sum == 0.0f ? kLowest : moved ? fmaf(c.top[n], c.q[n].factor, -(float)kLeastUnit) : c.base[n];
       const int column = first + n * 16 + i;
       if (column >= t.columns) continue;
       const int row = column / a.group, q_head = head * a.group + column - row * a.group;

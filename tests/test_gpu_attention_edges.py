@@ -167,3 +167,48 @@ def test_large_scores_of_which_one_is_the_largest(dtype, q_size, k_size, scale, 
         # the other weights are nothing in any precision (e^-200 and less)
         assert (np.abs(got - want) <= ref.tolerance(want, np.full_like(off, 16 * 2.0 ** -24), spread, dtype)).all(), at
         assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 60, 2.0 ** 80, 2.0 ** 94])
+@pytest.mark.parametrize("n,new,scratch", [(200, 1, 0), (600, 4, 0), (150, 40, 0), (4000, 1, 1 << 22)])
+def test_values_of_nothing_next_to_the_largest(size, n, new, scratch):
+    """Positions whose values are zeros count in the sum of the weights, before and behind values of any size."""
+    rng = np.random.default_rng(7)
+    for part in (slice(0, n // 2), slice(n // 2, n), slice(0, n - 3), slice(0, n, 2)):
+        cache, pages, tables = filled_cache(rng, "bf16", 128, 1, 16, [n])
+        v = round16((rng.standard_normal((n, 1, 128)) * size).astype(np.float32), "bf16")
+        v[part] = 0
+        p = np.arange(n)
+        pages.write(1, tables[0, p // 16] * 16 + p % 16, normal(rng, (n, 1, 128), "bf16"), v)
+        cache.put(pages)
+        q = normal(rng, (new, 2, 128), "bf16")
+        hints = (new, n)
+        assert not scratch or slices_of(cache, tables, new, 2, hints, scratch) > 1
+        out, lse = attend(cache, tables, [0, new], [n], bits16(q.reshape(new, -1), "bf16"), 2, 0.01, scratch=scratch, hints=hints)
+        want, want_lse, off, spread = ref.attention(decode64(q, "bf16"), rows_of(pages, tables, 16), [0, new], [n], 2, 1, 0.01)
+        got = decode64(host16(out), "bf16").reshape(want.shape)
+        # what is held below 2^-31 of the largest value of the tile's rows is lost (here none is, but zeros)
+        assert (np.abs(got - want) <= ref.tolerance(want, off, spread, "bf16") + 2.0 ** -31 * np.abs(decode64(v, "bf16")).max()).all()
+        assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
+
+
+def test_a_large_value_of_no_weight_behind_constant_ones():
+    """A position that weighs nothing does not take the others' sums with it, however large its value."""
+    rng = np.random.default_rng(8)
+    n = 300
+    for size in (1.0, 2.0 ** 70, 2.0 ** 94):
+        for at in (0, 150, n - 1):
+            cache, pages, tables = filled_cache(rng, "bf16", 128, 1, 16, [n])
+            k = np.broadcast_to(round16(rng.choice((-1.0, 1.0), 128).astype(np.float32), "bf16"), (n, 1, 128)).copy()
+            q = round16(np.broadcast_to(decode64(k[0, 0], "bf16").astype(np.float32), (1, 2, 128)), "bf16")
+            k[at] ^= 0x8000
+            v = np.broadcast_to(round16(np.float32([5.0]), "bf16"), (n, 1, 128)).copy()
+            v[at] = round16((rng.standard_normal((1, 128)) * size).astype(np.float32), "bf16")
+            p = np.arange(n)
+            pages.write(1, tables[0, p // 16] * 16 + p % 16, k, v)
+            cache.put(pages)
+            # scores of some 192 and -192: the one weighs e^-384, times 2^94 nothing
+            out, lse = attend(cache, tables, [0, 1], [n], bits16(q.reshape(1, -1), "bf16"), 2, 1.5)
+            assert (decode64(host16(out), "bf16") == 5.0).all(), (size, at)
+            _, want_lse, off, _ = ref.attention(decode64(q, "bf16"), rows_of(pages, tables, 16), [0, 1], [n], 2, 1, 1.5)
+            assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
