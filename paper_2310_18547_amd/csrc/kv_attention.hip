@@ -641,8 +641,8 @@ struct Shared {
   float4 stats[4][16 * NT];  // worth of a weight of 1 in powers of two, sum of weights, of weights times minima
 };
 
-// A tile's columns.  The four waves are 2^groups_log2 groups, of which each takes 16 NT columns (or, HEADS, all columns of a head of its own, from
-// `first_head` on); the waves of a group take the steps in turn and meet in LDS.
+// A tile's columns.  The four waves are 2^groups_log2 groups, of which each takes 16 NT columns; the waves of a group take the steps in turn and meet in
+// LDS.  HEADS (groups_log2 is 2): every wave takes all columns of a head of its own, from `first_head` on.
 template <class DT, int D, int NT, bool HEADS, bool ONCE>
 __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& t, int columns, int first_head, int groups_log2, int slice, Shared<D, NT>& shared) {
   constexpr int PER = 16 * NT;
@@ -689,12 +689,12 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
         put_sum(a, of_slice.whole, t.first_row + row, q_head, slice, base, sum);
     }
   }
-  if (groups_log2 == 2) return;
+  if (HEADS || groups_log2 == 2) return;
   __syncthreads();
   // sixteen threads to a column
-  const int waves = 4 >> groups_log2, part = threadIdx.x & 15, all = HEADS ? min(a.at.n_kv_heads - first_head, 1 << groups_log2) * columns : columns;
-  for (int j = threadIdx.x >> 4; j < all; j += 16) {
-    const int from = HEADS ? j / columns : j / PER, at = HEADS ? j - from * columns : j % PER;
+  const int waves = 4 >> groups_log2, part = threadIdx.x & 15;
+  for (int j = threadIdx.x >> 4; j < columns; j += 16) {
+    const int from = j / PER, at = j % PER;
     float base = kLowest;
     for (int w = 0; w < waves; ++w) base = fmaxf(base, shared.stats[(w << groups_log2) + from][at].x);
     float sum = 0.0f, minima = 0.0f, v[D / 16] = {};
@@ -709,7 +709,7 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const Tile& 
     }
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) v[k] += minima;
-    const int column = t.first_column + (HEADS ? at : j), row = column / a.group, q_head = (HEADS ? first_head + from : first_head) * a.group + column - row * a.group;
+    const int column = t.first_column + j, row = column / a.group, q_head = first_head * a.group + column - row * a.group;
     put_values<DT, D>(a, of_slice.whole, t.first_row + row, q_head, slice, part * (D / 16), v, sum);
     if (part == 0) put_sum(a, of_slice.whole, t.first_row + row, q_head, slice, base, sum);
   }
