@@ -212,3 +212,81 @@ def test_a_large_value_of_no_weight_behind_constant_ones():
             assert (decode64(host16(out), "bf16") == 5.0).all(), (size, at)
             _, want_lse, off, _ = ref.attention(decode64(q, "bf16"), rows_of(pages, tables, 16), [0, 1], [n], 2, 1, 1.5)
             assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
+
+
+# ---------------------------------------------------------------------------------------------- slices
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("d,heads,kv_heads,lens,new,window,hints", [
+    (128, 4, 2, [6000], [1], 1000, (1, 6000)), (64, 3, 3, [5000], [2], 777, (2, 5000)),
+    # ragged: requests of one slice, of some, without rows or positions; more rows and positions than the hint says
+    (128, 4, 2, [4100, 2500, 1, 0, 600, 33], [1, 1, 1, 1, 0, 1], 1500, (1, 4100)), (64, 4, 1, [3000, 700], [4, 1], 900, (4, 1200)),
+    (64, 2, 2, [3000, 2000], [2, 9], 1300, (2, 3000)),
+    # prompts behind long contexts
+    (128, 10, 2, [3000, 2200], [40, 40], 1000, (40, 3000)), (64, 4, 4, [2600, 40, 0, 333, 64], [40, 40, 1, 1, 64], 1111, (40, 2600))])
+def test_windows_in_slices(dtype, causal, d, heads, kv_heads, lens, new, window, hints):
+    """The slices of a row that a window lets see the last positions alone: the first step is not 0, and slices count from it."""
+    scratch = 1 << 24
+    assert plan_slices(dtype, d, heads, kv_heads, 16, lens, new, hints, scratch, window) > 1
+    a = check_attention(dtype, d, heads, kv_heads, 16, lens, new, causal, window, scratch=scratch, hints=hints, seed=31)
+    b = check_attention(dtype, d, heads, kv_heads, 16, lens, new, causal, window, scratch=scratch, hints=hints, seed=31)
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_tiny_scores_and_hidden_pages_in_slices(dtype):
+    """All weights alike, those of pages that are not of the cache nothing: whole slices of them, and the ends of others."""
+    rng = np.random.default_rng(32)
+    n, hints, scratch = 3000, (1, 3000), 1 << 22
+    cache, pages, tables = filled_cache(rng, dtype, 128, 1, 16, [n])
+    gone = np.r_[3, 40:75, 187]
+    tables[0, gone] = -1
+    assert slices_of(cache, tables, 1, 2, hints, scratch) > 1
+    size, scale = (1e-36, 1e-20) if dtype == "bf16" else (1e-6, 1e-30)
+    q = normal(rng, (1, 2, 128), dtype, size)
+    out, lse = attend(cache, tables, [0, 1], [n], bits16(q.reshape(1, -1), dtype), 2, scale, scratch=scratch, hints=hints)
+    hidden = lambda r: np.isin(np.arange(n) // 16, gone)  # noqa: E731
+    want, want_lse, off, spread = ref.attention(decode64(q, dtype), rows_of(pages, tables, 16), [0, 1], [n], 2, 1, scale, hidden=hidden)
+    got = decode64(host16(out), dtype).reshape(want.shape)
+    assert (np.abs(got - want) <= ref.tolerance(want, off, spread, dtype)).all()
+    assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
+
+
+def test_calls_in_slices_that_share_a_workspace_in_a_graph():
+    """Two captured calls and an eager one use one workspace, one after the other, over replays: each has slices and a join."""
+    rng = np.random.default_rng(33)
+    lens, hints, nbytes = [3000, 2500], (1, 3000), 1 << 21
+    cache, pages, tables = filled_cache(rng, "f16", 128, 2, 16, lens)
+    q = bits16(normal(rng, (2, 1024), "f16"), "f16")
+    scales = (0.05, 0.3)
+    want = [attend(cache, tables, [0, 1, 2], lens, q, 8, s, scratch=nbytes, hints=hints) for s in scales]
+    q_starts, kv_lens, t = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"), torch.tensor(lens, dtype=torch.int32, device="cuda"), \
+        torch.tensor(tables, device="cuda").int()
+    b = sg.make_kv_batch(2, 2, tables.shape[1], q_starts, kv_lens, t, max_q_len=1, max_kv_len=3000)
+    plan = sg.sgmv_plan_attention_q4(cache.c, b, 8, 0, 1 << 8, nbytes)
+    assert plan.slices > 1 and plan.launches == 2
+    work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    outs, sums = [torch.zeros(2, 1024, dtype=torch.float16, device="cuda") for _ in scales], [torch.zeros(2, 8, device="cuda") for _ in scales]
+
+    def call(i, stream):
+        sg.sgmv_attention_q4(cache.c, b, 1, outs[i], sums[i], q, 8, 1024, 1024, scales[i], 1, 0, work, nbytes, stream)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call(0, stream)
+            call(1, stream)
+    for i in range(5):
+        for x in (*outs, *sums, work):
+            x.fill_(7)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graph.replay()
+        if i % 2:  # the same workspace eagerly behind the replay
+            outs[0].record_stream(stream)
+            call(0, stream)
+        torch.cuda.synchronize()
+        for (out, lse), got, got_lse in zip(want, outs, sums):
+            assert torch.equal(got, out) and torch.equal(got_lse, lse), i
