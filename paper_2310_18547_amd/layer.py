@@ -149,10 +149,10 @@ class KvCacheQ4:
         self.scratch = torch.empty(max(self.scratch_bytes, 256), dtype=torch.uint8, device=device)
 
     def _scratch_bytes(self) -> int:
-        """Room for the slices of decode steps and of steps as the hints tell, whichever is more."""
-        least = B.make_kv_batch(self.n_reqs, min(self.n_tokens, self.n_reqs), self.width, None, None, None, max_q_len=1,
-                                max_kv_len=self.batch.max_kv_len)
-        return max(B.sgmv_attention_workspace_bytes(self.cache, b, self.n_heads, self.window) for b in (self.batch, least))
+        """Room for the slices of any step of single tokens, over contexts as long as the tables take, and of steps as the hints tell now.  Every
+        row of the cache counts, live or not, so that a cache of many more rows than requests divides the contexts of single tokens less."""
+        single = B.make_kv_batch(self.n_reqs, self.n_tokens, self.width, None, None, None, max_q_len=1)
+        return max(B.sgmv_attention_workspace_bytes(self.cache, b, self.n_heads, self.window) for b in (self.batch, single))
 
     def hint(self, max_q_len: int, max_kv_len: int) -> None:
         """Most rows that a request brings and most positions that one has, from here on (0: unknown); speed alone depends on them."""

@@ -119,3 +119,47 @@ def test_a_step_that_the_pages_do_not_suffice_for():
     cache.step(torch.tensor([1, 1, 0], dtype=torch.int32, device="cuda"))
     cache.run(0, *kv)
     assert int(cache.status[0]) == 0 and cache.check() == sg.KV_NO_PAGES and bool((cache.out[:2] != 5.0).all()) and bool((cache.out[2] == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("window", [0, 1500])
+def test_prompts_and_single_tokens_over_long_contexts_of_shared_heads(dtype, window):
+    """A cache of more rows than requests, eight heads over two: prompts in parts, then decode steps whose contexts are divided into slices."""
+    import paper_2310_18547_amd as sg
+    from paper_2310_18547_amd.layer import KvCacheQ4
+    rng = np.random.default_rng(17)
+    d, heads, kv_heads, rows, most = 128, 8, 2, 900, 2600
+    cache = KvCacheQ4(sg.F16 if dtype == "f16" else sg.BF16, d, heads, kv_heads, 1, 64, 64, 2, rows, most, window=window, max_q_len=rows)
+    table, held, lens = cache.rope_table.cpu().numpy(), [[[], []], [[], []]], np.zeros(2, int)
+    steps = [[900, 0], [800, 100], [750, 150], [1, 1], [1, 0], [1, 1]]
+    for new in steps:
+        cache.hint(max(new), int((lens + new).max()))
+        plan = sg.sgmv_plan_attention_q4(cache.cache, cache.batch, heads, window, cache.scratch, cache.scratch_bytes)
+        if max(new) == 1:
+            assert plan.kernel == sg.KERNEL_ATTENTION_FEW and plan.slices > 1
+        cache.step(torch.tensor(new, dtype=torch.int32, device="cuda"))
+        q, k, v = (torch.from_numpy(rng.standard_normal((rows, h * d)).astype(np.float32)).cuda().to(KIND[dtype]) for h in (heads, kv_heads, kv_heads))
+        cache.out.fill_(-3.0)
+        out = cache.run(0, q, k, v)
+        n, starts = sum(new), np.concatenate(([0], np.cumsum(new)))
+        at = np.concatenate([lens[r] + np.arange(new[r]) for r in range(2)]).astype(int)
+        lens += new
+        hq, hk, hv = (host16(x).reshape(rows, -1, d)[:n] for x in (q, k, v))
+        tq, tk = (ref.rotate(x, dtype, table, at, d, 0) for x in (hq, hk))
+        for r in range(2):
+            held[r][0].append(tk[starts[r]:starts[r + 1]])
+            held[r][1].append(hv[starts[r]:starts[r + 1]])
+        assert cache.lens.tolist() == lens.tolist() and bool((out[n:] == -3.0).all())
+        if max(new) > 1:
+            continue
+
+        def of(r, positions):
+            both = []
+            for x in held[r]:
+                codes, s, m = ref.quantize(np.concatenate(x), dtype)
+                both.append(codes * decode64(s, dtype)[..., None] + decode64(m, dtype)[..., None])
+            return both
+        want, _, off, spread = ref.attention(decode64(tq, dtype), of, starts, lens, heads, kv_heads, d ** -0.5, True, window)
+        got = decode64(host16(out), dtype).reshape(rows, heads, d)[:n]
+        assert (np.abs(got - want) <= ref.tolerance(want, off, spread, dtype)).all(), new
+    assert cache.check() == 0

@@ -78,3 +78,20 @@ def test_a_whole_layer(kv_calls):
         with pytest.raises(ValueError):
             layer.run(_rows(), residual, layer_idx, cache)
     assert len(kv_calls) == before and FFN > H
+
+
+@pytest.mark.parametrize("n_reqs,n_tokens,max_len,hints", [(1, 1, 131072, (0, 0)), (1, 1, 131072, (1, 500)), (1, 512, 131072, (1, 131072)),
+                                                           (1, 2048, 131072, (2048, 131072)), (64, 64, 4000, (1, 300)), (3, 700, 9000, (700, 9000))])
+@pytest.mark.parametrize("window", [0, 5000])
+def test_single_tokens_have_room_for_their_slices(n_reqs, n_tokens, max_len, hints, window):
+    """Whatever the hints were when the cache was made: a decode step's plan is that of a workspace without end."""
+    t = _cache(head_dim=128, n_heads=32, n_kv_heads=8, num_layers=1, n_reqs=n_reqs, n_tokens=n_tokens, max_len=max_len, max_q_len=hints[0],
+               max_kv_len=hints[1], window=window, rope_dim=0)
+    for longest in (0, max_len, max_len // 2, 400):
+        t.hint(1, longest)
+        own, free = (sg.sgmv_plan_attention_q4(t.cache, t.batch, 32, window, 1 << 8, n) for n in (t.scratch_bytes, 1 << 40))
+        assert (own.kernel, own.slices, own.workgroups) == (free.kernel, free.slices, free.workgroups), longest
+        assert t.scratch.numel() >= t.scratch_bytes
+    t.hint(1, max_len)
+    if window == 0 and n_reqs == 1:
+        assert sg.sgmv_plan_attention_q4(t.cache, t.batch, 32, 0, 1 << 8, t.scratch_bytes).slices >= 8
