@@ -270,8 +270,8 @@ __device__ __forceinline__ void load_query(const AttentionArgs& a, const uint16_
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
   out.sum = sum * 0x1p-20f;
-  // (not zero: times the -infinity of a hidden position that would be NaN)
-  out.factor = fits ? fmaxf(ldexpf(a.scale * 1.44269504088896341f, 20 - up), 0x1p-126f) : __uint_as_float(0x7FC00000u);
+  // (the power of two first: a scale near fp32's largest goes with small queries.  Not zero: times the -infinity of a hidden position that would be NaN)
+  out.factor = fits ? fmaxf(ldexpf(a.scale, 20 - up) * 1.44269504088896341f, 0x1p-126f) : __uint_as_float(0x7FC00000u);
 }
 
 // First of the values whose row 4 g + i of output tile j a lane receives: value_of + j.

@@ -7,7 +7,7 @@ import attention_reference as ref
 import paper_2310_18547_amd as sg
 from backbone_reference import round16
 from helpers import decode64
-from test_gpu_attention import attend, bits16, check_attention, filled_cache, host, host16, normal, rows_of
+from test_gpu_attention import Cache, attend, bits16, check_attention, filled_cache, host, host16, normal, rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -290,3 +290,40 @@ def test_calls_in_slices_that_share_a_workspace_in_a_graph():
         torch.cuda.synchronize()
         for (out, lse), got, got_lse in zip(want, outs, sums):
             assert torch.equal(got, out) and torch.equal(got_lse, lse), i
+
+
+# ---------------------------------------------------------------------------------------------- scales of the softmax and of rows at the ends of their types
+
+@pytest.mark.parametrize("q_size,scale", [(1e-37, 3.3e38), (1e-38, 3e38), (1e-30, 3.4e38), (1e-39, 1e38)])
+def test_softmax_scales_at_the_end_of_fp32(q_size, scale):
+    """A scale near fp32's largest, next to rows so small that the scores are ordinary or merely large."""
+    check_attention("bf16", 128, 4, 2, 16, [100, 37], [5, 1], q_size=q_size, scale=scale, seed=9)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_of_rows_of_every_size(dtype, d):
+    """Rows whose values lie anywhere in their type's range, its smallest numbers among them: bytes of the definition, and back."""
+    rng = np.random.default_rng(34)
+    n, heads = 400, 2
+    low, high = (-133, 126) if dtype == "bf16" else (-25, 15)
+    k, v = (round16((rng.standard_normal((n, heads, d)).clip(-1, 1) * 2.0 ** rng.integers(low, high, (n, heads, 1))).astype(np.float32), dtype) for _ in range(2))
+    k[::7, 0, 0] ^= 0x8000
+    cache = Cache(dtype, d, heads, 2, 16, n // 16)
+    slots = rng.permutation(n)
+    at = torch.tensor(slots, dtype=torch.int32, device="cuda")
+    b = sg.make_kv_batch(1, n, 1, None, None, None, at)
+    dk, dv = bits16(k, dtype), bits16(v, dtype)
+    sg.sgmv_kv_append_q4(cache.c, b, 1, None, None, dk, dv, heads, heads * d, heads * d, heads * d)
+    want = cache.reference()
+    want.write(1, slots, k, v)
+    # rows of zeros of both signs: the sign of a scale of 0, which meets codes of 0 and a minimum of +0, is that of one of them
+    got, held = cache.bytes(), want.bytes.copy()
+    for x in (got, held):
+        pairs = x[..., 16 * d:].view(np.uint16)
+        pairs[..., ::2][pairs[..., ::2] == 0x8000] = 0
+    assert np.array_equal(got, held)
+    back = [torch.zeros_like(dk), torch.zeros_like(dv)]
+    sg.sgmv_kv_read_q4(cache.c, 1, *back, heads * d, at, n)
+    for g, w in zip(back, want.rows(1, slots, fp32=True)):
+        assert np.array_equal(decode64(host16(g), dtype), decode64(round16(w, dtype), dtype))
