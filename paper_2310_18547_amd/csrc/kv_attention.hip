@@ -449,6 +449,9 @@ __device__ __forceinline__ void put_beside(const Held<D>& s, int lane, Beside<D>
 // Weights of a step and the weighted values.
 template <class DT, int D, int NT, bool MASKED>
 __device__ __forceinline__ void weigh_step(const Beside<D>& v, Scores<NT>& r, Columns<D, NT>& c) {
+  // Weights times scales as one binary16 number are off by 2^-12 of their size: an eighth of a bfloat16 result's own rounding (errors against 64 bits
+  // 0.0017 to 0.0018, with the rest as a second part 0.0017; single tokens take 1 to 3 % longer with it, two prompts of 4095 rows 16 %, 834 -> 969 us),
+  // and half of a binary16 result's, which has the second part.
   constexpr bool kTwoParts = std::is_same_v<DT, F16>;
   uint32_t high[NT][4], rest[NT][4];
   auto weigh = [&](auto which) {
@@ -782,9 +785,9 @@ __device__ __forceinline__ bool tile_by_work(const AttentionArgs& a, int columns
 
 // Up to 64 NT columns of one cache head (2^columns_log2; 2^7 where NT is 2).  grid = (cache heads x tiles, slices).
 //
-// Bound by the vector units, busy for 82 % of the time of two prompts of 4095 rows (the matrix cores for 29 %): a step of 32 positions takes a wave with 32
+// Bound by the vector units, busy for 81 % of the time of two prompts of 4095 rows (the matrix cores for 29 %): a step of 32 positions takes a wave with 32
 // columns some 320 instructions besides its 32 products, 126 of them for the codes of k and v whatever its columns.  8000 rows of 32 heads, 8 of the
-// cache, bfloat16 706 us (743 TFLOP/s), binary16, whose weights are two parts, 828; those two prompts, 64 heads, 8 of the cache, 826.  Four tiles of sixteen
+// cache, bfloat16 714 us (734 TFLOP/s), binary16, whose weights are two parts, 825 to 835; those two prompts, 64 heads, 8 of the cache, 834.  Four tiles of sixteen
 // columns to a wave would halve the codes' part: their 256 registers and more to a lane leave one wave to a SIMD, 2100 us.  Codes unpacked once for the
 // four waves, through LDS: a quarter fewer instructions, 877 us where this took 848, for a barrier a step.
 template <class DT, int D, int NT>
@@ -809,8 +812,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void attention_many_kernel(At
 // Requests of up to sixteen columns (more than the hint said: sixteen after sixteen), 2^HEADS_LOG2 cache heads to a workgroup.
 // grid = (cache heads / that x requests, slices).
 //
-// Bound by memory: 64 requests of 2048 positions, 32 heads, 571 MB, 98 us (5.9 TB/s, as a read of 1 GiB), of 512 to 2048 72.5 us (5.2; the last long ones are
-// alone), of 512 28.7; one of 130 000 positions, 8 heads, in 64 slices 29 us and 5 for their join.  Three waves to a SIMD: four (128 registers)
+// Bound by memory: 64 requests of 2048 positions, 32 heads, 571 MB, 98 us (5.9 TB/s, as a read of 1 GiB), of 512 to 2048 73 us (5.2; the last long ones are
+// alone), of 512 28.9; one of 130 000 positions, 8 heads, in 64 slices 29 us and 5 for their join.  Three waves to a SIMD: four (128 registers)
 // spill, two with two steps held at once are 3 % slower.
 template <class DT, int D, int HEADS_LOG2>
 __global__ __launch_bounds__(256, 3) void attention_few_kernel(AttentionArgs a, int first_request) {
