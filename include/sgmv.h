@@ -563,7 +563,8 @@ int sgmv_kv_read_q4(const sgmv_kv_cache* c, int32_t layer_idx, void* k, void* v,
  * Row j of a request with n rows stands at position kv_len - n + j; it sees the positions of its request up to its own (causal; all
  * of them without), and with a window only those after its own position - window.
  *   out         16-bit [n_tokens][n_heads][head_dim], row stride out_stride
- *   lse         fp32 [n_tokens][n_heads] or NULL: natural logarithm of the softmax's sum (to join parts of an attention)
+ *   lse         fp32 [n_tokens][n_heads] or NULL: natural logarithm of the softmax's sum (to join parts of an attention); off by
+ *               up to 2^-17 besides a score's roundings where v's values have no scale, by less where they have
  *   q           16-bit, row stride q_stride; n_heads a multiple of n_kv_heads
  *   scale       positive and finite (else SGMV_ERR_UNSUPPORTED)
  *   window      0: none

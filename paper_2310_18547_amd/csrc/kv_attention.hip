@@ -604,8 +604,10 @@ __device__ __forceinline__ float of_column(float v) {
   return v + __shfl_xor(v, 32);
 }
 
+// (The sum's exponent meets the base before its logarithm does: of the two, up to 90 each, little may be left.)
 __device__ __forceinline__ float log_sum(float base, float sum) {
-  return sum == 0.0f ? -__uint_as_float(0x7F800000u) : (base + log2f(sum)) * 0.693147180559945309f;
+  const float exponent = (float)__builtin_amdgcn_frexp_expf(sum), rest = log2f(__builtin_amdgcn_frexp_mantf(sum));
+  return sum == 0.0f ? -__uint_as_float(0x7F800000u) : (base + exponent + rest) * 0.693147180559945309f;
 }
 
 // What the sum of a row's first slice is where that slice has been written as the row's result.

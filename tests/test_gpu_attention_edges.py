@@ -214,6 +214,22 @@ def test_a_large_value_of_no_weight_behind_constant_ones():
             assert (np.abs(host(lse) - want_lse) <= off + 2.0 ** -22 * (1 + np.abs(want_lse))).all()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads", [1, 7])
+def test_logarithms_of_sums_of_equal_weights(dtype, heads):
+    """Zero queries over any number of positions whose values are zeros: the logarithm of that number.  Sums of ones are exact, so that the logarithm's own
+    rounding (two of its last places, which are of at most 2^-23 next to 1), its product with ln 2 and two additions are all that is off."""
+    lens = [*range(1, 40), 100, 555, 1000, 2047, 3000]
+    cache = Cache(dtype, 64, 1, 2, 16, 190, fill=0)  # codes, scales and minima of zeros
+    tables = np.broadcast_to(np.arange(190), (len(lens), 190)).copy()
+    q = np.zeros((len(lens), heads, 64), np.uint16)
+    for scratch, hints in ((0, (1, 0)), (1 << 24, (1, 3000)), (0, (40, 0))):
+        out, lse = attend(cache, tables, np.arange(len(lens) + 1), lens, bits16(q.reshape(len(lens), -1), dtype), heads, 0.125, scratch=scratch, hints=hints)
+        want = np.log(np.array(lens, np.float64))[:, None]
+        assert (host(out.float()) == 0).all()
+        assert (np.abs(host(lse) - want) <= 2.0 ** -22 + 2.0 ** -22 * want).all(), (scratch, hints, np.abs(host(lse) - want).max())
+
+
 # ---------------------------------------------------------------------------------------------- slices
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
