@@ -574,7 +574,7 @@ int sgmv_kv_read_q4(const sgmv_kv_cache* c, int32_t layer_idx, void* k, void* v,
  * A row that sees nothing is zeros, its lse -inf.  Sums, maxima and the softmax are fp32; the codes are exact in the matrix cores, q
  * keeps all its bits next to its row's largest value, and the weights w * s enter as one 16-bit part with 11 bits for bfloat16, two for
  * binary16 (what v holds below 2^-30 of the largest scale among the positions that a row or its neighbours in a tile see, or, of
- * bfloat16, below 2^-111, gets lost).  Rows of q that hold a NaN, an infinity or a value of 2^100 and more are NaN where a position is theirs to see (on a page of the
+ * bfloat16, below 2^-111, gets lost).  Rows of q that hold a NaN, an infinity or a value of 2^100 (times scale: some 2^120) and more are NaN where a position is theirs to see (on a page of the
  * cache or not); so is what sees a position that holds a NaN or an infinity, and what sees one of 2^100 and more, or whose scores pass 2^120, may be.  But for that limit,
  * positions that a row does not see do not matter, whatever they hold.  Scores are fp32 numbers, with their roundings.
  * The order of the sums depends on the hints and the workspace, not on the run: same

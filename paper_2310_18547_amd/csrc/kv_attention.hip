@@ -252,8 +252,6 @@ __device__ __forceinline__ void load_query(const AttentionArgs& a, const uint16_
   top = max(top, (uint32_t)__shfl_xor((int)top, 16));
   top = max(top, (uint32_t)__shfl_xor((int)top, 32));
   const float largest = decode1<DT>((uint16_t)top);
-  // not finite, or 2^100 and more: the column is NaN, whatever its operands
-  const bool fits = largest < 0x1p100f;
   const int up = 13 - ((int)(__float_as_uint(largest) >> 23) - 127);
   float sum = 0.0f;
 #pragma unroll
@@ -271,7 +269,10 @@ __device__ __forceinline__ void load_query(const AttentionArgs& a, const uint16_
   sum += __shfl_xor(sum, 32);
   out.sum = sum * 0x1p-20f;
   // (the power of two first: a scale near fp32's largest goes with small queries.  Not zero: times the -infinity of a hidden position that would be NaN)
-  out.factor = fits ? fmaxf(ldexpf(a.scale, 20 - up) * 1.44269504088896341f, 0x1p-126f) : __uint_as_float(0x7FC00000u);
+  const float factor = ldexpf(a.scale, 20 - up) * 1.44269504088896341f;
+  // not finite, or 2^100 and more, with the scale 2^120 and more: the column is NaN, whatever its operands
+  const bool fits = largest < 0x1p100f && factor < __uint_as_float(0x7F800000u);
+  out.factor = fits ? fmaxf(factor, 0x1p-126f) : __uint_as_float(0x7FC00000u);
 }
 
 // First of the values whose row 4 g + i of output tile j a lane receives: value_of + j.

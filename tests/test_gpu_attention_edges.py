@@ -316,6 +316,31 @@ def test_softmax_scales_at_the_end_of_fp32(q_size, scale):
     check_attention("bf16", 128, 4, 2, 16, [100, 37], [5, 1], q_size=q_size, scale=scale, seed=9)
 
 
+@pytest.mark.parametrize("q_power,scale_power,fits", [(5, 114, True), (5, 117, False), (60, 59, True), (60, 63, False), (98, -20, True)])
+def test_queries_times_the_scale(q_power, scale_power, fits):
+    """Rows that times the scale pass 2^120 are NaN where they see positions; others take keys as small as their scores need."""
+    rng = np.random.default_rng(10)
+    n, d = 60, 128
+    cache, pages, tables = filled_cache(rng, "bf16", d, 1, 16, [n])
+    k = round16((rng.choice((-1.0, 1.0), (1, 1, d)) * 2.0 ** (10.0 - q_power - scale_power)).astype(np.float32), "bf16")
+    p = np.arange(n)
+    pages.write(1, tables[0, p // 16] * 16 + p % 16, np.broadcast_to(k, (n, 1, d)), normal(rng, (n, 1, d), "bf16"))
+    cache.put(pages)
+    # one value at the power itself, the others below it; rows 0 and 1 stand in front of position 0
+    q = round16((2.0 ** q_power * np.where(np.arange(d) == 9, 1.0, rng.random((n + 2, 2, d)))).astype(np.float32), "bf16")
+    scale = 2.0 ** scale_power
+    out, lse = attend(cache, tables, [0, n + 2], [n], bits16(q.reshape(n + 2, -1), "bf16"), 2, scale)
+    got, sums = decode64(host16(out), "bf16").reshape(n + 2, 2, d), host(lse)
+    assert (got[:2] == 0).all() and np.isneginf(sums[:2]).all()
+    if not fits:
+        assert np.isnan(got[2:]).all() and np.isnan(sums[2:]).all()
+        return
+    want, want_lse, off, spread = ref.attention(decode64(q, "bf16"), rows_of(pages, tables, 16), [0, n + 2], [n], 2, 1, scale)
+    # keys of the same bytes: scores that are the same to the bit
+    assert (np.abs(got - want) <= ref.tolerance(want, np.full_like(off, (n + 16) * 2.0 ** -24), spread, "bf16")).all()
+    assert (np.abs(sums[2:] - want_lse[2:]) <= off[2:] + 2.0 ** -17 + 2.0 ** -22 * (1 + np.abs(want_lse[2:]))).all()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_append_of_rows_of_every_size(dtype, d):
