@@ -450,9 +450,9 @@ __device__ __forceinline__ void put_beside(const Held<D>& s, int lane, Beside<D>
 // Weights of a step and the weighted values.
 template <class DT, int D, int NT, bool MASKED>
 __device__ __forceinline__ void weigh_step(const Beside<D>& v, Scores<NT>& r, Columns<D, NT>& c) {
-  // Weights times scales as one binary16 number are off by 2^-12 of their size: an eighth of a bfloat16 result's own rounding (errors against 64 bits
+  // Weights times scales as one binary16 number are off by up to 2^-11 of their size: an eighth of a bfloat16 result's own rounding (errors against 64 bits
   // 0.0017 to 0.0018, with the rest as a second part 0.0017; single tokens take 1 to 3 % longer with it, two prompts of 4095 rows 16 %, 834 -> 969 us),
-  // and half of a binary16 result's, which has the second part.
+  // and as much as a binary16 result's, which has the second part.
   constexpr bool kTwoParts = std::is_same_v<DT, F16>;
   uint32_t high[NT][4], rest[NT][4];
   auto weigh = [&](auto which) {
